@@ -105,7 +105,9 @@ enum {
   SB_CALL_LEAF_VALUES = 6,
   SB_CALL_GRADIENTS = 7,
   SB_CALL_UPDATE_PREDICTIONS = 8,
-  SB_CALL_UPDATE_AND_GRADIENTS = 9
+  SB_CALL_UPDATE_AND_GRADIENTS = 9,
+  SB_CALL_LOG_PROBS = 10,
+  SB_CALL_DISTILL = 11  /* sb_distill_loss and sb_distill_gradients */
 };
 
 /* Losses of sb_gradients (the cross-entropies of the paper's experiments). */
@@ -113,6 +115,22 @@ enum {
   SB_LOSS_SOFTMAX_CE = 0,  /* multiclass: softmax cross-entropy, one label per row */
   SB_LOSS_SIGMOID_BCE = 1  /* multilabel: binary cross-entropy per output, sigmoid link */
 };
+
+/* Element types and orders of the scores of sb_log_probs. */
+enum { SB_F32 = 0, SB_F16 = 1, SB_BF16 = 2 };
+enum {
+  SB_COLUMN_MAJOR = 0, /* (i, j) at F[j*ld_f + i], ld_f >= n: the scores of this library (fp32) */
+  SB_ROW_MAJOR = 1     /* (i, j) at F[i*ld_f + j], ld_f >= d: the logits of a network */
+};
+
+/* What the values of a teacher's list are (sb_distill_loss, sb_distill_gradients). */
+enum {
+  SB_TEACHER_LOGITS = 0,   /* scores: the teacher's distribution is the softmax of the list at the call's temperature */
+  SB_TEACHER_LOG_PROBS = 1 /* log probabilities, at the call's temperature already; what the list leaves out is dropped */
+};
+
+/* Longest list of alternatives per row (sb_log_probs) and longest teacher's list. */
+#define SB_MAX_TOP 64
 
 /* Text of the last non-OK status returned on this thread ("" if none). */
 const char* sb_last_error(void);
@@ -126,8 +144,9 @@ int32_t sb_abi_version(void);
  * included).  n_nodes: nodes of the level (BUILD_HISTOGRAMS,
  * SCORE_SPLITS, PARTITION_ROWS), leaves (LEAF_VALUES).  depth: tree depth
  * (GROW_TREE).  d: output dimension (SKETCH, LEAF_VALUES, GRADIENTS,
- * UPDATE_AND_GRADIENTS; the LEAF_VALUES size covers all three hessian
- * forms).  UPDATE_PREDICTIONS needs only n.  Returns -1 (and sets the error
+ * UPDATE_AND_GRADIENTS, LOG_PROBS, DISTILL; the LEAF_VALUES size covers all
+ * three hessian forms).  k: sketch columns, alternatives (LOG_PROBS, 0..64),
+ * list length (DISTILL, 1..64).  UPDATE_PREDICTIONS needs only n.  Returns -1 (and sets the error
  * text) for sizes outside the range the call itself accepts (n < 2^31, m and
  * d <= 65535, k <= 255, n_bins in [2, 256], nodes as documented per call).
  * sb_layout_bins and sb_subtract_histograms need no workspace.
@@ -476,6 +495,91 @@ int32_t sb_update_and_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
                                 const int32_t* labels, const uint8_t* Y, int64_t ld_y, float* G, int64_t ld_g,
                                 float* hess, int64_t ld_hess, float* h_row, double* norm2, void* ws,
                                 int64_t ws_bytes, void* stream);
+
+/*
+ * sb_log_probs -- what a model answers for every row of scores: the log
+ * probability and the rank of a given class, the log normaliser, the entropy
+ * and the most probable classes, under p = softmax(a / temperature) of the
+ * row's d scores a.
+ *
+ * F, dtype, order, ld_f  n x d scores; SB_COLUMN_MAJOR takes SB_F32 only,
+ *            SB_ROW_MAJOR every type.  -inf excludes a class (p = 0).  A row
+ *            with NaN or +inf gets NaN for logp, lse and entropy.
+ * temperature  in [1e-4, 1e4].
+ * labels     int32, n entries: the given class of every row (may be NULL
+ *            if logp and rank are).
+ * logp       out (may be NULL): n fp32, log p of the given class; 0 for a
+ *            label outside [0, d), so that such rows add nothing to a sum.
+ * rank       out (may be NULL): n int32, the classes before the given one by
+ *            (score descending, class ascending), 0 = the best; -1 for a label
+ *            outside [0, d).
+ * lse        out (may be NULL): n fp32, log sum_j exp(a_j / temperature).
+ * entropy    out (may be NULL): n fp32, -sum_j p_j log p_j.
+ * k          0..SB_MAX_TOP alternatives per row (0: none; may exceed d).
+ * top_id, top_logp, ld_top  out (k > 0): alternative t of row i at
+ *            [t*ld_top + i], ld_top >= n: class and log p, ordered by
+ *            (score descending, class ascending).  Classes of score -inf are no
+ *            alternatives: the places past the last one get class -1 and
+ *            -inf.  This is the teacher's list of the distillation calls.
+ * A row whose scores are all -inf gets lse = logp = -inf and entropy 0.
+ * Sums in fp32 of terms at the row's maximum; ranks and the order of the
+ * alternatives compare the scores as given, so they are exact.
+ * Workspace: sb_workspace_bytes(SB_CALL_LOG_PROBS, n, d, k).
+ */
+int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f,
+                     double temperature, const int32_t* labels, float* logp, int32_t* rank, float* lse, float* entropy,
+                     int32_t k, int32_t* top_id, float* top_logp, int64_t ld_top, void* ws, int64_t ws_bytes,
+                     void* stream);
+
+/*
+ * sb_distill_loss -- distillation loss of every row against a teacher's top
+ * classes, mixed with the cross-entropy of a label.
+ *
+ * For a row with scores a, p1 = softmax(a), pT = softmax(a / T) and the
+ * teacher's list of (class c_t, value z_t), t < k:
+ *   SB_TEACHER_LOGITS     q_t = softmax of z_t / T over the list,
+ *   SB_TEACHER_LOG_PROBS  q_t = exp(z_t);
+ *   loss = w (-log p1[label]) + (1 - w) T^2 sum_t q_t (log q_t - log pT[c_t]),
+ * w = hard_weight.  Places whose class is outside [0, d) are unused whatever
+ * their value; a value of -inf has q_t = 0; a class may be listed twice.  Rows
+ * whose label is outside [0, d) have no first term, rows with no used place
+ * no second.
+ *
+ * F, ld_f      n x d fp32 scores, column-major, finite.
+ * temperature  T, in [1e-4, 1e4].  hard_weight in [0, 1].
+ * labels       n int32; may be NULL if hard_weight is 0.
+ * teacher      SB_TEACHER_*.
+ * k, t_id, t_val, ld_t  1..SB_MAX_TOP places per row: place t of row i at
+ *              [t*ld_t + i], ld_t >= n (as sb_log_probs writes them).
+ * loss         out: n fp32.
+ * fp32 arithmetic, sums in a fixed order.
+ * Workspace: sb_workspace_bytes(SB_CALL_DISTILL, n, d, k).
+ */
+int32_t sb_distill_loss(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature, double hard_weight,
+                        const int32_t* labels, int32_t teacher, int32_t k, const int32_t* t_id, const float* t_val,
+                        int64_t ld_t, float* loss, void* ws, int64_t ws_bytes, void* stream);
+
+/*
+ * sb_distill_gradients -- first and second derivatives of that loss by the
+ * scores, in the form of sb_gradients:
+ *   G[j*ld_g + i]  = w (p1_j - [j == label]) + (1 - w) T (Q pT_j - sum_{t: c_t == j} q_t),
+ *   hess           = w p1_j (1 - p1_j) + (1 - w) Q pT_j (1 - pT_j)   (the diagonal),
+ * Q = sum_t q_t (1 for logits), w = 0 in the terms that the row lacks (a row
+ * that has neither gets zeros).
+ *
+ * loss     out (may be NULL): n fp32, as sb_distill_loss up to rounding.
+ * G        out: n x d fp32, column-major, ld_g >= n.
+ * hess     out (may be NULL): n x d fp32, column-major, ld_hess >= n.
+ * h_row    out (may be NULL): n fp32 row means of the hessians.
+ * norm2    out (may be NULL): d fp64 values sum_i G[i, j]^2 of the stored G,
+ *          added in a fixed order (deterministic).
+ * F, G and hess must not overlap.  Every other argument as sb_distill_loss.
+ */
+int32_t sb_distill_gradients(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature,
+                             double hard_weight, const int32_t* labels, int32_t teacher, int32_t k,
+                             const int32_t* t_id, const float* t_val, int64_t ld_t, float* loss, float* G,
+                             int64_t ld_g, float* hess, int64_t ld_hess, float* h_row, double* norm2, void* ws,
+                             int64_t ws_bytes, void* stream);
 
 /*
  * Kernel timing for benchmarks.  Between sb_profile_begin() and

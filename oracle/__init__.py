@@ -26,6 +26,8 @@ Modules
             objective they minimise.
 ``boost``   loss derivatives (eq. 2) of softmax and sigmoid cross-entropy,
             the prediction update and the boosting loop (Section 2).
+``scores``  log probabilities, ranks, entropies and best classes of score rows,
+            and the distillation loss with its derivatives.
 
 Parity status: every function is pinned by the non-GPU tests
 (``tests/test_oracle_*.py``) except the exact values of the random draws
@@ -53,3 +55,4 @@ from .split import (  # noqa: F401
 from .brute import brute_best_split, brute_tree, exact_region_score  # noqa: F401
 from .leaf import leaf_rows, leaf_values, leaf_objective  # noqa: F401
 from . import boost  # noqa: F401
+from . import scores  # noqa: F401

@@ -21,9 +21,15 @@ SB_OK, SB_E_ARG, SB_E_SHAPE, SB_E_UNSUPPORTED, SB_E_DEVICE = 0, 1, 2, 3, 4
 SB_SKETCH_TOP_OUTPUTS, SB_SKETCH_RANDOM_SAMPLING, SB_SKETCH_RANDOM_PROJECTION, SB_SKETCH_IDENTITY = 0, 1, 2, 3
 (SB_CALL_SKETCH, SB_CALL_BUILD_HISTOGRAMS, SB_CALL_SCORE_SPLITS, SB_CALL_PARTITION_ROWS, SB_CALL_GROW_TREE,
  SB_CALL_HIST_EXPONENTS, SB_CALL_LEAF_VALUES, SB_CALL_GRADIENTS, SB_CALL_UPDATE_PREDICTIONS,
- SB_CALL_UPDATE_AND_GRADIENTS) = range(10)
+ SB_CALL_UPDATE_AND_GRADIENTS, SB_CALL_LOG_PROBS, SB_CALL_DISTILL) = range(12)
 SB_LOSS_SOFTMAX_CE, SB_LOSS_SIGMOID_BCE = 0, 1
 LOSS = {"softmax": SB_LOSS_SOFTMAX_CE, "sigmoid": SB_LOSS_SIGMOID_BCE}
+SB_F32, SB_F16, SB_BF16 = 0, 1, 2
+DTYPE = {"f32": SB_F32, "f16": SB_F16, "bf16": SB_BF16}
+SB_COLUMN_MAJOR, SB_ROW_MAJOR = 0, 1
+SB_TEACHER_LOGITS, SB_TEACHER_LOG_PROBS = 0, 1
+TEACHER = {"logits": SB_TEACHER_LOGITS, "log_probs": SB_TEACHER_LOG_PROBS}
+SB_MAX_TOP = 64
 
 KIND = {
     "top_outputs": SB_SKETCH_TOP_OUTPUTS,
@@ -53,6 +59,9 @@ SYMBOLS = (
     "sb_gradients",
     "sb_update_predictions",
     "sb_update_and_gradients",
+    "sb_log_probs",
+    "sb_distill_loss",
+    "sb_distill_gradients",
     "sb_profile_begin",
     "sb_profile_end",
 )
@@ -98,6 +107,11 @@ _PROTOS["sb_leaf_values_from_loss"] = (_I32, [_I32, _P, _I64, _I32, _I64, _P, _P
 _PROTOS["sb_update_predictions"] = (_I32, [_P, _I64, _I32, _I64, _P, _P, _I32, _P, _I64, _F64, _P, _I64, _P])
 _PROTOS["sb_update_and_gradients"] = (_I32, [_I32, _P, _I64, _I32, _I64, _P, _P, _I32, _P, _I64, _F64, _P, _P, _I64,
                                              _P, _I64, _P, _I64, _P, _P, _P, _I64, _P])
+_PROTOS["sb_log_probs"] = (_I32, [_P, _I32, _I32, _I64, _I32, _I64, _F64, _P, _P, _P, _P, _P, _I32, _P, _P, _I64, _P, _I64,
+                                  _P])
+_PROTOS["sb_distill_loss"] = (_I32, [_P, _I64, _I32, _I64, _F64, _F64, _P, _I32, _I32, _P, _P, _I64, _P, _P, _I64, _P])
+_PROTOS["sb_distill_gradients"] = (_I32, [_P, _I64, _I32, _I64, _F64, _F64, _P, _I32, _I32, _P, _P, _I64, _P, _P, _I64,
+                                          _P, _I64, _P, _P, _P, _I64, _P])
 _PROTOS["sb_profile_begin"] = (_I32, [])
 _PROTOS["sb_profile_end"] = (_I32, [ctypes.POINTER(ctypes.c_double), ctypes.POINTER(ctypes.c_int64)])
 
@@ -260,6 +274,28 @@ def sb_update_and_gradients(loss, F, n, d, ld_f, row_idx, leaf_off, n_leaves, V,
                                                  _ptr(V), ld_v, lr, _ptr(labels), _ptr(Y), ld_y, _ptr(G), ld_g,
                                                  _ptr(hess), ld_hess, _ptr(h_row), _ptr(norm2), _ptr(ws), ws_bytes,
                                                  _stream(stream)))
+
+
+def sb_log_probs(F, dtype, order, n, d, ld_f, temperature, labels, logp, rank, lse, entropy, k, top_id, top_logp, ld_top,
+                 ws, ws_bytes, stream=None):
+    return _check(load().sb_log_probs(_ptr(F), dtype, order, n, d, ld_f, temperature, _ptr(labels), _ptr(logp),
+                                      _ptr(rank), _ptr(lse), _ptr(entropy), k, _ptr(top_id), _ptr(top_logp), ld_top,
+                                      _ptr(ws), ws_bytes, _stream(stream)))
+
+
+def sb_distill_loss(F, n, d, ld_f, temperature, hard_weight, labels, teacher, k, t_id, t_val, ld_t, loss, ws, ws_bytes,
+                    stream=None):
+    return _check(load().sb_distill_loss(_ptr(F), n, d, ld_f, temperature, hard_weight, _ptr(labels), teacher, k,
+                                         _ptr(t_id), _ptr(t_val), ld_t, _ptr(loss), _ptr(ws), ws_bytes,
+                                         _stream(stream)))
+
+
+def sb_distill_gradients(F, n, d, ld_f, temperature, hard_weight, labels, teacher, k, t_id, t_val, ld_t, loss, G, ld_g,
+                         hess, ld_hess, h_row, norm2, ws, ws_bytes, stream=None):
+    return _check(load().sb_distill_gradients(_ptr(F), n, d, ld_f, temperature, hard_weight, _ptr(labels), teacher, k,
+                                              _ptr(t_id), _ptr(t_val), ld_t, _ptr(loss), _ptr(G), ld_g, _ptr(hess),
+                                              ld_hess, _ptr(h_row), _ptr(norm2), _ptr(ws), ws_bytes,
+                                              _stream(stream)))
 
 
 def sb_profile_begin():

@@ -205,6 +205,12 @@ int64_t sb_workspace_bytes(int32_t call, int64_t n, int32_t m, int32_t n_bins, i
     case SB_CALL_LEAF_VALUES:
       if (n < 1 || n > MAX_ROWS || d < 1 || d > 65535 || n_nodes < 1 || n_nodes > MAX_LEAVES) break;
       return leaf_ws_bytes(n, d, n_nodes);
+    case SB_CALL_LOG_PROBS:
+      if (n < 1 || n > MAX_ROWS || d < 1 || d > 65535 || k < 0 || k > SB_MAX_TOP) break;
+      return log_probs_ws_bytes(n, d, k);
+    case SB_CALL_DISTILL:
+      if (n < 1 || n > MAX_ROWS || d < 1 || d > 65535 || k < 1 || k > SB_MAX_TOP) break;
+      return distill_ws_bytes(n, d, k);
     default:
       set_error("sb_workspace_bytes: unknown call id");
       return -1;
@@ -648,6 +654,108 @@ int32_t sb_update_and_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
   if (rc) return rc;
   return launch_update_gradients(loss, F, n, d, ld_f, row_idx, leaf_off, n_leaves, V, ld_v, lr, labels, Y, ld_y, G,
                                  ld_g, hess, ld_hess, h_row, norm2, ws, static_cast<hipStream_t>(stream));
+}
+
+}  // extern "C"
+
+namespace {
+
+// Leading dimensions up to here: byte offsets of 65535 columns stay in 64 bits.
+constexpr int64_t MAX_LD = int64_t(1) << 44;
+
+bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
+  const uintptr_t a0 = reinterpret_cast<uintptr_t>(a), b0 = reinterpret_cast<uintptr_t>(b);
+  return a && b && a0 < b0 + (uintptr_t)b_bytes && b0 < a0 + (uintptr_t)a_bytes;
+}
+
+bool temperature_ok(double t) { return t >= 1e-4 && t <= 1e4; }
+
+int32_t check_distill(const char* call, const DistillArgs& a) {
+  const std::string c(call);
+  if (a.teacher != SB_TEACHER_LOGITS && a.teacher != SB_TEACHER_LOG_PROBS)
+    return fail(SB_E_UNSUPPORTED, c + ": unknown teacher kind " + std::to_string(a.teacher));
+  if (!a.F || !a.t_id || !a.t_val) return fail(SB_E_ARG, c + ": F, t_id and t_val must not be NULL");
+  if (a.n < 1 || a.n > MAX_ROWS) return fail(SB_E_ARG, c + ": n must be in [1, 2^31)");
+  if (a.d < 1 || a.d > 65535) return fail(SB_E_ARG, c + ": d must be in [1, 65535]");
+  if (a.k < 1 || a.k > SB_MAX_TOP) return fail(SB_E_ARG, c + ": k must be in [1, 64]");
+  if (!temperature_ok(a.T)) return fail(SB_E_ARG, c + ": temperature must be in [1e-4, 1e4]");
+  if (!(a.w >= 0.0 && a.w <= 1.0)) return fail(SB_E_ARG, c + ": hard_weight must be in [0, 1]");
+  if (a.w > 0.0 && !a.labels) return fail(SB_E_ARG, c + ": a hard_weight above 0 needs labels");
+  if (a.ld_f < a.n || a.ld_f > MAX_LD) return fail(SB_E_SHAPE, c + ": ld_f must be >= n");
+  if (a.ld_t < a.n || a.ld_t > MAX_LD) return fail(SB_E_SHAPE, c + ": ld_t must be >= n");
+  if (!aligned(a.F, 4) || !aligned(a.t_id, 4) || !aligned(a.t_val, 4))
+    return fail(SB_E_SHAPE, c + ": F, t_id and t_val must be 4-byte aligned");
+  return SB_OK;
+}
+
+}  // namespace
+
+extern "C" {
+
+int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f,
+                     double temperature, const int32_t* labels, float* logp, int32_t* rank, float* lse, float* entropy,
+                     int32_t k, int32_t* top_id, float* top_logp, int64_t ld_top, void* ws, int64_t ws_bytes,
+                     void* stream) {
+  const std::string c("sb_log_probs");
+  if (dtype != SB_F32 && dtype != SB_F16 && dtype != SB_BF16)
+    return fail(SB_E_UNSUPPORTED, c + ": unknown element type " + std::to_string(dtype));
+  if (order != SB_COLUMN_MAJOR && order != SB_ROW_MAJOR)
+    return fail(SB_E_UNSUPPORTED, c + ": unknown order " + std::to_string(order));
+  if (order == SB_COLUMN_MAJOR && dtype != SB_F32)
+    return fail(SB_E_UNSUPPORTED, c + ": column-major scores are fp32");
+  if (!F) return fail(SB_E_ARG, c + ": F must not be NULL");
+  if (n < 1 || n > MAX_ROWS) return fail(SB_E_ARG, c + ": n must be in [1, 2^31)");
+  if (d < 1 || d > 65535) return fail(SB_E_ARG, c + ": d must be in [1, 65535]");
+  if (k < 0 || k > SB_MAX_TOP) return fail(SB_E_ARG, c + ": k must be in [0, 64]");
+  if (!temperature_ok(temperature)) return fail(SB_E_ARG, c + ": temperature must be in [1e-4, 1e4]");
+  if ((logp || rank) && !labels) return fail(SB_E_ARG, c + ": logp and rank need labels");
+  if (k > 0 && (!top_id || !top_logp)) return fail(SB_E_ARG, c + ": k > 0 needs top_id and top_logp");
+  if (!logp && !rank && !lse && !entropy && k == 0) return fail(SB_E_ARG, c + ": no output asked for");
+  if (ld_f > MAX_LD || ld_f < (order == SB_COLUMN_MAJOR ? n : d))
+    return fail(SB_E_SHAPE, c + ": ld_f must be >= n (column-major) or >= d (row-major)");
+  if (k > 0 && (ld_top < n || ld_top > MAX_LD)) return fail(SB_E_SHAPE, c + ": ld_top must be >= n");
+  if (!aligned(F, dtype == SB_F32 ? 4 : 2)) return fail(SB_E_SHAPE, c + ": F must be aligned to its element type");
+  const int32_t rc = need_ws(ws, ws_bytes, log_probs_ws_bytes(n, d, k), "sb_log_probs");
+  if (rc) return rc;
+  return launch_log_probs(F, dtype, order, n, d, ld_f, temperature, logp || rank ? labels : nullptr, logp, rank, lse,
+                          entropy, k, top_id, top_logp, ld_top, ws, static_cast<hipStream_t>(stream));
+}
+
+int32_t sb_distill_loss(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature, double hard_weight,
+                        const int32_t* labels, int32_t teacher, int32_t k, const int32_t* t_id, const float* t_val,
+                        int64_t ld_t, float* loss, void* ws, int64_t ws_bytes, void* stream) {
+  const char* call = "sb_distill_loss";
+  const DistillArgs a{F, n, d, ld_f, temperature, hard_weight, labels, teacher, k, t_id, t_val, ld_t,
+                      loss, nullptr, 0, nullptr, 0, nullptr, nullptr};
+  int32_t rc = check_distill(call, a);
+  if (rc) return rc;
+  if (!loss) return fail(SB_E_ARG, "sb_distill_loss: loss must not be NULL");
+  rc = need_ws(ws, ws_bytes, distill_ws_bytes(n, d, k), call);
+  if (rc) return rc;
+  return launch_distill(a, ws, static_cast<hipStream_t>(stream), call);
+}
+
+int32_t sb_distill_gradients(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature,
+                             double hard_weight, const int32_t* labels, int32_t teacher, int32_t k,
+                             const int32_t* t_id, const float* t_val, int64_t ld_t, float* loss, float* G,
+                             int64_t ld_g, float* hess, int64_t ld_hess, float* h_row, double* norm2, void* ws,
+                             int64_t ws_bytes, void* stream) {
+  const char* call = "sb_distill_gradients";
+  const std::string c(call);
+  const DistillArgs a{F, n, d, ld_f, temperature, hard_weight, labels, teacher, k, t_id, t_val, ld_t,
+                      loss, G, ld_g, hess, ld_hess, h_row, norm2};
+  int32_t rc = check_distill(call, a);
+  if (rc) return rc;
+  if (!G) return fail(SB_E_ARG, c + ": G must not be NULL");
+  if (ld_g < n || ld_g > MAX_LD) return fail(SB_E_SHAPE, c + ": ld_g must be >= n");
+  if (hess && (ld_hess < n || ld_hess > MAX_LD)) return fail(SB_E_SHAPE, c + ": ld_hess must be >= n");
+  const int64_t fb = ((int64_t)(d - 1) * ld_f + n) * 4, gb = ((int64_t)(d - 1) * ld_g + n) * 4;
+  const int64_t hb = hess ? ((int64_t)(d - 1) * ld_hess + n) * 4 : 0;
+  if (overlap(F, fb, G, gb) || overlap(F, fb, hess, hb) || overlap(G, gb, hess, hb))
+    return fail(SB_E_SHAPE, c + ": F, G and hess overlap");
+  rc = need_ws(ws, ws_bytes, distill_ws_bytes(n, d, k), call);
+  if (rc) return rc;
+  return launch_distill(a, ws, static_cast<hipStream_t>(stream), call);
 }
 
 }  // extern "C"

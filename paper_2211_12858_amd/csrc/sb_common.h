@@ -231,6 +231,36 @@ int32_t launch_update_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
                                 const int32_t* labels, const uint8_t* Y, int64_t ld_y, float* G, int64_t ld_g,
                                 float* hess, int64_t ld_hess, float* h_row, double* norm2, void* ws, hipStream_t st);
 
+int64_t log_probs_ws_bytes(int64_t n, int32_t d, int32_t k);
+int32_t launch_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f, double T,
+                         const int32_t* labels, float* logp, int32_t* rank, float* lse, float* entropy, int32_t k,
+                         int32_t* top_id, float* top_logp, int64_t ld_top, void* ws, hipStream_t st);
+
+// One distillation call; G is NULL for the loss alone.
+struct DistillArgs {
+  const float* F;
+  int64_t n;
+  int32_t d;
+  int64_t ld_f;
+  double T;
+  double w;  // weight of the label's cross-entropy
+  const int32_t* labels;
+  int32_t teacher;
+  int32_t k;
+  const int32_t* t_id;
+  const float* t_val;
+  int64_t ld_t;
+  float* loss;
+  float* G;
+  int64_t ld_g;
+  float* hess;
+  int64_t ld_h;
+  float* h_row;
+  double* norm2;
+};
+int64_t distill_ws_bytes(int64_t n, int32_t d, int32_t k);
+int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const char* call);
+
 // ---------------------------------------------------------------- profiling
 // Event pairs around histogram-kernel launches while profiling is on (per thread).
 bool profile_on();

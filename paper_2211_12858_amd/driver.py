@@ -16,8 +16,14 @@ The sketch lives row-major in ``GH[i, t]``, each row padded to a multiple of
 8 floats so that it fills whole 32-byte sectors.  ``step()`` runs one
 tree: the sketch (once per tree) and the depth-wise level loop, entirely on
 the device; ``leaf_values()`` then gives the tree's leaf values from the
-full gradient matrix.  No computation happens in Python.
+full gradient matrix.  ``log_probs`` says what rows of scores answer: log
+probabilities, ranks, entropies and the best classes, which are also the lists
+that ``Booster`` with the loss "distill" learns from.  No computation happens in
+Python.
 """
+import contextlib
+from typing import NamedTuple, Optional
+
 import numpy as np
 import torch
 
@@ -44,6 +50,68 @@ def record_stride(m):
             s *= 2
         return s
     return _round_up(need, 128)
+
+
+class LogProbs(NamedTuple):
+    """What rows of scores answer (sb_log_probs): logp and rank are None without labels, the lists without k."""
+    logp: Optional[torch.Tensor]      # (n,) float32: log probability of the label
+    rank: Optional[torch.Tensor]      # (n,) int32: classes before the label, 0 = the best
+    lse: torch.Tensor                 # (n,) float32: log normaliser
+    entropy: torch.Tensor             # (n,) float32
+    top_id: Optional[torch.Tensor]    # (k, n) int32: the best classes, best first; -1 past the last
+    top_logp: Optional[torch.Tensor]  # (k, n) float32: their log probabilities
+
+
+_SCORE_TYPES = {torch.float32: L.SB_F32, torch.float16: L.SB_F16, torch.bfloat16: L.SB_BF16}
+
+
+@contextlib.contextmanager
+def _on(device, stream):
+    """The device of the data as the current one, and the stream (a torch stream, a raw hipStream_t or None for the
+    device's current one) as its current stream, so that what is allocated here is not reused before the work on it."""
+    with torch.cuda.device(device):
+        if isinstance(stream, int):
+            stream = torch.cuda.ExternalStream(stream, device=device) if stream else torch.cuda.default_stream(device)
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            yield
+
+
+def _check_vector(name, t, n, dtype, device):
+    if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or t.device != device:
+        raise ValueError("%s must be %d contiguous elements of %s on %s" % (name, n, dtype, device))
+
+
+def log_probs(scores, labels=None, k=0, temperature=1.0, order="column", stream=None):
+    """Log probabilities of the labels, ranks, log normalisers, entropies and the k best classes of rows of scores.
+
+    scores: a (d, n) float32 tensor with order="column" (the booster's scores), an (n, d) float32, float16 or bfloat16
+    tensor with order="row" (a network's logits); the last dimension contiguous.  labels: (n,) int32.  Returns
+    :class:`LogProbs` of new tensors on the scores' device."""
+    if order not in ("column", "row"):
+        raise ValueError("order must be 'column' or 'row'")
+    if scores.dim() != 2 or scores.dtype not in _SCORE_TYPES or scores.numel() == 0:
+        raise ValueError("scores must be a matrix of float32, float16 or bfloat16")
+    rows, inner = scores.shape
+    ld = scores.stride(0) if rows > 1 else inner
+    if (inner > 1 and scores.stride(1) != 1) or ld < inner:
+        raise ValueError("the last dimension of the scores must be contiguous")
+    n, d = (inner, rows) if order == "column" else (rows, inner)
+    dev = scores.device
+    if labels is not None:
+        _check_vector("labels", labels, n, torch.int32, dev)
+    with _on(dev, stream):
+        def new(dtype, *shape):
+            return torch.empty(shape, dtype=dtype, device=dev)
+
+        ws = workspace(L.sb_workspace_bytes(L.SB_CALL_LOG_PROBS, n=n, d=d, k=k), dev)
+        r = LogProbs(logp=None if labels is None else new(torch.float32, n),
+                     rank=None if labels is None else new(torch.int32, n),
+                     lse=new(torch.float32, n), entropy=new(torch.float32, n),
+                     top_id=new(torch.int32, k, n) if k else None, top_logp=new(torch.float32, k, n) if k else None)
+        L.sb_log_probs(scores, _SCORE_TYPES[scores.dtype], L.SB_COLUMN_MAJOR if order == "column" else L.SB_ROW_MAJOR, n, d,
+                       ld, temperature, labels, r.logp, r.rank, r.lse, r.entropy, k, r.top_id, r.top_logp, n, ws,
+                       ws.numel())
+    return r
 
 
 class SplitSearch:
@@ -234,6 +302,10 @@ class Booster:
        (``sb_update_and_gradients``); reading ``F`` (or ``flush()``) applies a
        held update on its own (``sb_update_predictions``).
 
+    The loss "distill" learns from a teacher's lists (``set_teacher``): step 1 is
+    ``sb_distill_gradients``, which also stores the hessians that step 4 reads,
+    after the held update; the split-search weight is 1 as for softmax.
+
     F, G and the hessians are (d, n) float32 device tensors (column-major).
     """
 
@@ -252,6 +324,8 @@ class Booster:
         self.ws_upd_grad = workspace(L.sb_workspace_bytes(L.SB_CALL_UPDATE_AND_GRADIENTS, n=n, d=d), dev)
         self.labels = None
         self.Y = None
+        self.hess = torch.empty((d, n), dtype=torch.float32, device=dev) if loss == "distill" else None
+        self.teacher = None
         self.pending = None  # leaf values of the last tree, not yet added to F
 
     @property
@@ -270,14 +344,60 @@ class Booster:
 
     def set_target(self, target):
         """Labels (n,) int32 for softmax, or a (d, n) uint8 0/1 matrix for sigmoid (device tensors)."""
+        if self.loss == "distill":
+            raise ValueError("the loss 'distill' takes its targets by set_teacher")
         if self.loss == "softmax":
             self.labels = target
         else:
             self.Y = target
 
+    def set_teacher(self, t_id, t_val, values="log_probs", temperature=1.0, labels=None, hard_weight=0.0):
+        """The teacher's lists that the loss "distill" learns from, and how (sb_distill_loss).
+
+        t_id, t_val: (k, n) int32 classes and float32 values, as ``log_probs`` returns them (device tensors; places of
+        class -1 are unused); values: "log_probs" (at this temperature) or "logits"; labels: (n,) int32, needed for a
+        hard_weight above 0."""
+        if self.loss != "distill":
+            raise ValueError("only the loss 'distill' has a teacher")
+        k = t_id.shape[0] if t_id.dim() == 2 else 0
+        for t, dtype in ((t_id, torch.int32), (t_val, torch.float32)):
+            if t.shape != (k, self.n) or t.dtype != dtype or not t.is_contiguous() or t.device != self._F.device:
+                raise ValueError("the lists must be (k, n) contiguous int32 and float32 tensors on the booster's device")
+        if labels is not None:
+            _check_vector("labels", labels, self.n, torch.int32, self._F.device)
+        elif hard_weight > 0:
+            raise ValueError("a hard_weight above 0 needs labels")
+        ws = workspace(L.sb_workspace_bytes(L.SB_CALL_DISTILL, n=self.n, d=self.d, k=k), self._F.device)
+        self.teacher = (float(temperature), float(hard_weight), labels, L.TEACHER[values], k, t_id, t_val, ws)
+
+    def _teacher(self):
+        if self.teacher is None:
+            raise ValueError("the loss 'distill' needs set_teacher first")
+        return self.teacher
+
+    def distill_loss(self, stream=None):
+        """The distillation loss of every row at the current scores: a new (n,) float32 tensor."""
+        T, w, y, kind, k, t_id, t_val, ws = self._teacher()
+        self.flush(stream)
+        with _on(self._F.device, stream):
+            loss = torch.empty(self.n, dtype=torch.float32, device=self._F.device)
+            L.sb_distill_loss(self._F, self.n, self.d, self.n, T, w, y, kind, k, t_id, t_val, self.n, loss, ws, ws.numel())
+        return loss
+
+    def log_probs(self, labels=None, k=0, temperature=1.0, stream=None):
+        """What the current scores answer (:func:`log_probs`)."""
+        self.flush(stream)
+        return log_probs(self._F, labels, k, temperature, "column", stream)
+
     def gradients(self, stream=None):
         """Derivatives at the current scores (a held update is applied first, in the same pass)."""
         n, d = self.n, self.d
+        if self.loss == "distill":
+            T, w, y, kind, k, t_id, t_val, ws = self._teacher()
+            self.flush(stream)
+            L.sb_distill_gradients(self._F, n, d, n, T, w, y, kind, k, t_id, t_val, n, None, self.G, n, self.hess, n, None,
+                                   self.norm2, ws, ws.numel(), stream)
+            return
         h_row = self.h_row if self.loss == "sigmoid" else None
         if self.pending is not None:
             V = self.pending
@@ -291,8 +411,11 @@ class Booster:
 
     def step(self, u=None, Pi=None, stream=None):
         self.gradients(stream)
-        h = self.ones if self.loss == "softmax" else self.h_row
+        h = self.h_row if self.loss == "sigmoid" else self.ones
         self.ss.sketch(self.kind, self.G, h, u=u, Pi=Pi, stream=stream, norm2_in=self.norm2)
         self.ss.grow(stream)
         # the tree's leaf segments stay in ss.row_idx / ss.leaf_off until the next grow
+        if self.loss == "distill":
+            self.pending = self.ss.leaf_values(self.G, self.hess, stream=stream)
+            return
         self.pending = self.ss.leaf_values_from_loss(self.loss, self.G, self.labels, self.Y, stream=stream)
