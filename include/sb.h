@@ -573,6 +573,7 @@ int32_t sb_distill_loss(const float* F, int64_t n, int32_t d, int64_t ld_f, doub
  * h_row    out (may be NULL): n fp32 row means of the hessians.
  * norm2    out (may be NULL): d fp64 values sum_i G[i, j]^2 of the stored G,
  *          added in a fixed order (deterministic).
+ * Probabilities below 2^-126 of the row's largest are taken as 0.
  * F, G and hess must not overlap.  Every other argument as sb_distill_loss.
  */
 int32_t sb_distill_gradients(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature,

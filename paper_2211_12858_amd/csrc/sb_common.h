@@ -219,6 +219,8 @@ int32_t launch_leaf_values_from_loss(int32_t loss, const float* G, int64_t n, in
                                      const int32_t* leaf_off, int32_t n_leaves, double lambda, double* V, int64_t ld_v,
                                      void* ws, hipStream_t st);
 int64_t grad_ws_bytes(int64_t n, int32_t d);
+// norm2[j] = the sum of column j's partials npart[j * parts ..], in a fixed order.
+void launch_norm_final(const double* npart, int32_t d, int32_t parts, double* norm2, hipStream_t st);
 int32_t launch_gradients(int32_t loss, const float* F, int64_t n, int32_t d, int64_t ld_f, const int32_t* labels,
                          const uint8_t* Y, int64_t ld_y, float* G, int64_t ld_g, float* hess, int64_t ld_hess,
                          float* h_row, double* norm2, void* ws, hipStream_t st);

@@ -1,0 +1,70 @@
+// Work split of the distillation kernels (host side, from the shape alone: no HIP
+// call), so that the order of the norms' sums does not depend on the device.
+#ifndef SB_DISTILL_PLAN_H_
+#define SB_DISTILL_PLAN_H_
+#include <cstdint>
+
+namespace sb {
+
+constexpr int DISTILL_MAX_WAVES = 16;
+constexpr int DISTILL_REGS_MAX_D = 1024;
+// lane offsets of the two-part waves are 32-bit byte offsets of up to 63 columns
+constexpr int64_t DISTILL_PARTS_MAX_LD = int64_t(1) << 24;
+constexpr int DISTILL_RED = 8;  // per-wave values that a block's waves exchange
+
+// Rows in the registers of a block's waves.
+struct DistillPlan {
+  int rows;    // rows per tile: 64 x c columns per wave, or 32 x 2c past 512 columns
+  int c;       // columns per lane
+  int waves;   // waves per row tile
+  int groups;  // row tiles per block
+  int tiles;
+  int grid;
+  int lds;     // bytes per block
+};
+
+constexpr int distill_tile_floats(int c) { return 64 * ((c < 16 ? c : 16) + 4); }
+
+constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
+  DistillPlan p{};
+  p.rows = d <= 512 ? 64 : 32;
+  p.c = d <= 8 ? 8 : d <= 256 ? 16 : 32;
+  const int cols = p.c * (64 / p.rows);
+  p.waves = (d + cols - 1) / cols;
+  p.groups = p.waves == 1 ? 4 : p.waves == 2 ? 2 : 1;
+  p.lds = p.groups * 4 * (2 * k * p.rows + DISTILL_RED * p.waves * 64 + p.waves * distill_tile_floats(p.c));
+  const int64_t rows = (int64_t)p.rows * p.groups;
+  p.tiles = (int)((n + rows - 1) / rows);
+  // blocks that fit on 256 CUs at once by waves and LDS, all with the same number of tiles but the last ones
+  int per_cu = 16 / (p.waves * p.groups);
+  const int by_lds = 160 * 1024 / p.lds;
+  if (per_cu > by_lds) per_cu = by_lds;
+  if (per_cu < 1) per_cu = 1;
+  int most = 256 * per_cu;
+  if (most > p.tiles) most = p.tiles;
+  const int per = (p.tiles + most - 1) / most;
+  p.grid = (p.tiles + per - 1) / per;
+  return p;
+}
+
+// Wider rows (and leading dimensions that the lanes' offsets do not cover): the
+// statistics of column ranges first, then the outputs range by range.
+constexpr int DISTILL_RANGE = 512;  // columns per block, 128 per wave
+constexpr int DISTILL_SLOTS = 256;  // row tiles in flight, and norm partials per column at most
+
+struct DistillWidePlan {
+  int ranges;
+  int tiles;  // of 64 rows
+  int slots;
+};
+
+constexpr DistillWidePlan distill_wide_plan(int64_t n, int32_t d) {
+  DistillWidePlan p{};
+  p.ranges = (d + DISTILL_RANGE - 1) / DISTILL_RANGE;
+  p.tiles = (int)((n + 63) / 64);
+  p.slots = p.tiles < DISTILL_SLOTS ? p.tiles : DISTILL_SLOTS;
+  return p;
+}
+
+}  // namespace sb
+#endif

@@ -764,6 +764,10 @@ int launch_softmax_wide(GradArgs a, hipStream_t st) {
 
 }  // namespace
 
+void launch_norm_final(const double* npart, int32_t d, int32_t parts, double* norm2, hipStream_t st) {
+  hipLaunchKernelGGL(k_grad_norm_final, dim3((d + 3) / 4), dim3(256), 0, st, npart, d, parts, norm2);
+}
+
 int64_t grad_ws_bytes(int64_t n, int32_t d) {
   const int64_t tiles = (n + GRAD_THREADS - 1) / GRAD_THREADS;
   return align256((int64_t)d * (tiles < GRAD_PARTS ? tiles : GRAD_PARTS) * 8);
@@ -786,7 +790,7 @@ int32_t launch_gradients(int32_t loss, const float* F, int64_t n, int32_t d, int
     hipLaunchKernelGGL(k_grad<SB_LOSS_SOFTMAX_CE>, dim3(blocks), dim3(GRAD_THREADS), 0, st, a);
   else
     hipLaunchKernelGGL(k_grad<SB_LOSS_SIGMOID_BCE>, dim3(blocks), dim3(GRAD_THREADS), 0, st, a);
-  if (norm2) hipLaunchKernelGGL(k_grad_norm_final, dim3((d + 3) / 4), dim3(256), 0, st, npart, d, a.n_parts, norm2);
+  if (norm2) launch_norm_final(npart, d, a.n_parts, norm2, st);
   return check_launch("sb_gradients");
 }
 
@@ -849,7 +853,7 @@ int32_t launch_update_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
   } else {
     launch_softmax_regs<true>(a, (size_t)table, st);
   }
-  if (norm2) hipLaunchKernelGGL(k_grad_norm_final, dim3((d + 3) / 4), dim3(256), 0, st, npart, d, parts, norm2);
+  if (norm2) launch_norm_final(npart, d, parts, norm2, st);
   return check_launch("sb_update_and_gradients");
 }
 

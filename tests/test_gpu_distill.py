@@ -114,7 +114,9 @@ def check(F, t_id, t_val, T, w, labels, kind, fwd, got, rows=None):
         th[i] += 8 * U * h[i]
         tl[i] += U * (k + 8) * lmag
         lt[i] = lmag
-    tiny = 2.0 ** -140
+    # exponentials below 2^-126 of the row's largest are 0, as documented: p lacks at most 2^-126, g at most
+    # (w + (1 - w) T Q) 2^-126 and h no more, Q <= 64 here
+    tiny = 2.0 ** -126 * (1 + 64 * T)
 
     def close(name, gotv, want, tol):
         bad = ~(np.abs(gotv.astype(np.float64) - want) <= 2 * tol + tiny)
