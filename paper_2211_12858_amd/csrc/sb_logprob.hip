@@ -1,13 +1,27 @@
 // Log probability and rank of a given class, log normaliser, entropy and the
 // best classes of every row of scores (sb_log_probs).
 //
-// With m = max_j a_j and c = 1 / T, e_j = exp((a_j - m) c), s = sum e_j,
-// t = sum e_j (a_j - m) c:
-//   lse = m c + log s,  log p_y = (a_y - m) c - log s,  entropy = log s - t / s
+// With m = max_j a_j, c2 = log2(e) / T, y_j = (a_j - m) c2, e_j = 2^y_j,
+// s = sum e_j, t = sum e_j y_j:
+//   lse = m / T + log s,  log p_y = (a_y - m) / T - log s,
+//   entropy = log s - ln 2 t / s
 // (log s >= 0 >= t, so the entropy has no cancellation).
+//
+// k_rows_by_lane: one lane per row, the columns in order, 16 at a time: a running
+//   maximum, the two sums rescaled when it grows, and the best classes so far as a
+//   sorted list in registers; a score enters it if it is above the last one (equal
+//   scores stay behind the earlier class).  Column-major scores are read as runs of
+//   a column; row-major ones go through an LDS tile of 128 bytes of 64 rows.  Where
+//   there are few rows the columns are split over waves, and k_join joins the
+//   partial statistics and lists, one wave per row.
+// k_row_in_block (row-major): a row in the registers of a wave or of a block.  The
+//   k-th largest of 64 lane maxima bounds the k-th largest score from below; the
+//   scores not under it, seldom many more than k, are collected in LDS and ranked
+//   there by counting.
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
+#include <cfloat>
 #include <cmath>
 
 #include "sb_common.h"
@@ -15,12 +29,14 @@
 namespace sb {
 namespace {
 
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+
 struct LogProbArgs {
   const void* F;
   int64_t n;
   int32_t d;
-  int64_t rs, cs;  // element (i, j) at F[i * rs + j * cs]
-  float c;         // 1 / T
+  int64_t ld;
+  float c, c2;  // 1 / T, log2(e) / T
   const int32_t* labels;
   float* logp;
   int32_t* rank;
@@ -30,95 +46,578 @@ struct LogProbArgs {
   int32_t* top_id;
   float* top_logp;
   int64_t ld_top;
+  int tiles, splits, per;  // k_rows_by_lane: row tiles, column splits, columns per split
+  float* part;             // splits > 1: [split][4 + 2 k][n]: m, s, t, before, scores, classes
 };
 
+__device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float to_f32(float x) { return x; }
 __device__ inline float to_f32(__half x) { return __half2float(x); }
 __device__ inline float to_f32(__hip_bfloat16 x) { return __bfloat162float(x); }
 
-// One wave per row: the maximum, the sums and the rank, then the alternatives one
-// at a time, each the best class after the one before.
-template <typename T>
-__global__ void __launch_bounds__(256) k_log_probs(LogProbArgs a) {
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  if (row >= a.n) return;
-  const T* x = static_cast<const T*>(a.F) + row * a.rs;
-  float m = -INFINITY;
-  for (int j = lane; j < a.d; j += 64) m = fmaxf(m, to_f32(x[j * a.cs]));
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  const float mm = m == -INFINITY ? 0.0f : m;
-  const int y = a.labels ? a.labels[row] : -1;
+__device__ inline void wave_sync() {
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(0xc07f);
+  __builtin_amdgcn_wave_barrier();
+  asm volatile("" ::: "memory");
+}
+
+// The row's real outputs from its statistics.  m starts at -FLT_MAX, so that a row of
+// -inf has s = 0 and no differences of infinities.
+struct RowStats {
+  float m, s, t;
+  __device__ float log_s() const { return logf(s); }
+};
+__device__ inline void store_row(const LogProbArgs& a, int64_t row, const RowStats& r, int y, float ay, int before) {
+  const float ls = r.log_s();
+  const bool none = r.s == 0.0f;
   const bool has = y >= 0 && y < a.d;
-  const float ay = has ? to_f32(x[y * a.cs]) : 0.0f;
+  if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(r.m, a.c, ls);
+  if (a.entropy) a.entropy[row] = none ? 0.0f : ls - LN2 * r.t / r.s;
+  if (a.logp) a.logp[row] = !has ? 0.0f : none ? -INFINITY : (ay - r.m) * a.c - ls;
+  if (a.rank) a.rank[row] = has ? before : -1;
+}
+__device__ inline void store_top(const LogProbArgs& a, int64_t row, int place, float v, int id, const RowStats& r,
+                                 float ls) {
+  a.top_id[place * a.ld_top + row] = id;
+  a.top_logp[place * a.ld_top + row] = id < 0 ? -INFINITY : (v - r.m) * a.c - ls;
+}
+
+// ---------------------------------------------------------------- one lane per row
+constexpr int CH = 16;         // columns per step
+constexpr int TILE_B = 144;    // bytes of a row's 128 in the LDS tile: lanes' 16-byte reads fall on different banks
+
+template <int KM>
+struct LaneRow {
+  float m = -FLT_MAX, s = 0.0f, t = 0.0f;
+  int before = 0;
+  float v[KM ? KM : 1];
+  int id[KM ? KM : 1];
+
+  // Places past k start at +inf, in front, where nothing gets before them: the
+  // list's last place is the k-th.
+  __device__ void clear(int k) {
+#pragma unroll
+    for (int q = 0; q < KM; ++q) {
+      v[q] = q < KM - k ? INFINITY : -INFINITY;
+      id[q] = -1;
+    }
+  }
+  // x above the last place (or -inf: nothing changes): the places that it beats move on by one.
+  __device__ void insert(float x, int j) {
+    bool c[KM ? KM : 1];
+#pragma unroll
+    for (int q = 0; q < KM; ++q) c[q] = x > v[q];
+#pragma unroll
+    for (int q = KM - 1; q > 0; --q) {
+      v[q] = __builtin_amdgcn_fmed3f(v[q - 1], x, v[q]);
+      id[q] = c[q] ? (c[q - 1] ? id[q - 1] : j) : id[q];
+    }
+    v[0] = fmaxf(v[0], x);
+    id[0] = c[0] ? j : id[0];
+  }
+  // Columns j0 .. j0 + CH - 1 (those past the last are -inf); again(i) is column
+  // j0 + i once more, for i that differs from lane to lane.
+  template <typename Again>
+  __device__ void step(const LogProbArgs& a, const float (&x)[CH], int j0, int y, float ay, Again again) {
+    float mn = x[0];
+#pragma unroll
+    for (int i = 1; i < CH; ++i) mn = fmaxf(mn, x[i]);
+    const bool news = KM > 0 && mn > v[KM ? KM - 1 : 0];
+    mn = fmaxf(m, mn);
+    const float dy = fmaxf((m - mn) * a.c2, -1500.0f), f = exp2_hw(dy);
+    float as = 0.0f, at = 0.0f;
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const float yv = (x[i] - mn) * a.c2, e = exp2_hw(yv);
+      as += e;
+      at = fmaf(e, fmaxf(yv, -1500.0f), at);
+    }
+    t = fmaf(f, fmaf(s, dy, t), at);
+    s = fmaf(f, s, as);
+    m = mn;
+    if (a.rank) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) before += x[i] > ay || (x[i] == ay && j0 + i < y);
+    }
+    if (KM > 0 && __any(news)) {
+      // a bit per column above the list's last place, the first column highest;
+      // then the lanes' columns one after the other
+      const float last = v[KM ? KM - 1 : 0];
+      uint32_t bits = 0;
+#pragma unroll
+      for (int i = 0; i < CH; ++i) bits = 2 * bits + (x[i] > last);
+      while (__any(bits != 0)) {
+        const int i = CH - 32 + __builtin_clz(bits | 1);
+        const float xi = bits ? again(i) : -INFINITY;
+        insert(xi, j0 + i);
+        bits &= ~(1u << (CH - 1 - i));
+      }
+    }
+  }
+};
+
+template <int KM>
+__device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t row, int split, int y, float ay) {
+  if (a.splits == 1) {
+    const RowStats st{r.m, r.s, r.t};
+    store_row(a, row, st, y, ay, r.before);
+    const float ls = st.log_s();
+#pragma unroll
+    for (int q = 0; q < KM; ++q)
+      if (q >= KM - a.k) store_top(a, row, q - (KM - a.k), r.v[q], r.id[q], st, ls);
+    return;
+  }
+  float* p = a.part + (int64_t)split * (4 + 2 * a.k) * a.n + row;
+  p[0] = r.m;
+  p[a.n] = r.s;
+  p[2 * a.n] = r.t;
+  p[3 * a.n] = __int_as_float(r.before);
+#pragma unroll
+  for (int q = 0; q < KM; ++q)
+    if (q >= KM - a.k) {
+      p[(int64_t)(4 + q - (KM - a.k)) * a.n] = r.v[q];
+      p[(int64_t)(4 + a.k + q - (KM - a.k)) * a.n] = __int_as_float(r.id[q]);
+    }
+}
+
+constexpr int STEP_S = CH + 4;  // floats of a row's step in LDS
+
+template <int KM>
+__global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
+  __shared__ __align__(16) float lds[KM ? 4 : 1][KM ? 64 * STEP_S : 4];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t unit = (int64_t)blockIdx.x * 4 + w;
+  if (unit >= (int64_t)a.tiles * a.splits) return;
+  const int split = (int)(unit / a.tiles);
+  const int64_t base = (unit - (int64_t)split * a.tiles) * 64;
+  const int64_t left = a.n - 1 - base;  // rows past the end read row n - 1 and store nothing
+  const int loc = lane < left ? lane : (int)left;
+  const int64_t row = base + loc;
+  const int j0 = split * a.per, j1 = j0 + a.per < a.d ? j0 + a.per : a.d;
+  const float* F = static_cast<const float*>(a.F) + base;
+  const int y = a.labels ? a.labels[row] : -1;
+  const float ay = y >= 0 && y < a.d ? F[(int64_t)y * a.ld + loc] : 0.0f;
+  LaneRow<KM> r;
+  r.clear(a.k);
+  float x[CH], nx[CH];
+  auto load = [&](float (&to)[CH], int j) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) {
+      const int col = j + i < j1 ? j + i : j1 - 1;
+      to[i] = (F + (int64_t)col * a.ld)[loc];
+    }
+  };
+  load(nx, j0);
+  for (int j = j0; j < j1; j += CH) {
+#pragma unroll
+    for (int i = 0; i < CH; ++i) x[i] = j + i < j1 ? nx[i] : -INFINITY;
+    if (j + CH < j1) load(nx, j + CH);
+    // the lane's own 16 scores, for the few that enter its list
+    float* mine = lds[KM ? w : 0] + (KM ? lane * STEP_S : 0);
+    if (KM) {
+#pragma unroll
+      for (int i = 0; i < CH; i += 4)
+        *reinterpret_cast<float4*>(mine + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+    }
+    r.step(a, x, j, y, ay, [&](int i) { return mine[i]; });
+  }
+  if (lane <= left) finish_lane<KM>(a, r, row, split, y, ay);
+}
+
+// Row-major: 128 bytes of each of 64 rows at a time, eight lanes a row, through LDS.
+template <typename T, int KM>
+__global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
+  constexpr int VEC = 16 / sizeof(T), COLS = 8 * VEC;
+  __shared__ __align__(16) char lds[4][64 * TILE_B];
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t tile = (int64_t)blockIdx.x * 4 + w;
+  if (tile >= a.tiles) return;
+  const int64_t base = tile * 64;
+  const int64_t left = a.n - 1 - base;
+  const int loc = lane < left ? lane : (int)left;
+  const int64_t row = base + loc;
+  const T* F = static_cast<const T*>(a.F);
+  const int y = a.labels ? a.labels[row] : -1;
+  const float ay = y >= 0 && y < a.d ? to_f32(F[row * a.ld + y]) : 0.0f;
+  LaneRow<KM> r;
+  r.clear(a.k);
+  // lane l brings vector l % 8 of rows l / 8, l / 8 + 8, ...
+  const int vrow = lane >> 3, vcol = (lane & 7) * VEC;
+  char* put = lds[w] + vrow * TILE_B + (lane & 7) * 16;
+  const char* get = lds[w] + lane * TILE_B;
+  uint4 nx[8];
+  auto load = [&](int j) {
+    const int c = j + vcol;
+#pragma unroll
+    for (int q = 0; q < 8; ++q) {
+      const int rr = vrow + q * 8;
+      const T* p = F + (base + (rr < left ? rr : left)) * a.ld + c;
+      if (c + VEC <= a.d) {
+        __builtin_memcpy(&nx[q], p, 16);
+      } else {  // the row's end: its elements one by one
+        T e[VEC];
+#pragma unroll
+        for (int u = 0; u < VEC; ++u)
+          if (c + u < a.d) e[u] = p[u];
+        __builtin_memcpy(&nx[q], e, 16);
+      }
+    }
+  };
+  load(0);
+  for (int j = 0; j < a.d; j += COLS) {
+    wave_sync();
+#pragma unroll
+    for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(put + q * 8 * TILE_B) = nx[q];
+    wave_sync();
+    if (j + COLS < a.d) load(j + COLS);
+    for (int h = 0; h < COLS / CH; ++h) {
+      if (j + h * CH >= a.d) break;
+      float x[CH];
+#pragma unroll
+      for (int q = 0; q < CH / VEC; ++q) {
+        const uint4 raw = *reinterpret_cast<const uint4*>(get + (h * (CH / VEC) + q) * 16);
+        T e[VEC];
+        __builtin_memcpy(e, &raw, 16);
+#pragma unroll
+        for (int u = 0; u < VEC; ++u) x[q * VEC + u] = j + h * CH + q * VEC + u < a.d ? to_f32(e[u]) : -INFINITY;
+      }
+      r.step(a, x, j + h * CH, y, ay,
+             [&](int i) { return to_f32(reinterpret_cast<const T*>(get)[h * CH + i]); });
+    }
+  }
+  if (lane <= left) finish_lane<KM>(a, r, row, 0, y, ay);
+}
+
+// The splits' statistics and lists of one row joined by one wave, lane per split.
+__global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
+  const int lane = threadIdx.x & 63;
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
+  if (row >= a.n) return;
+  const bool on = lane < a.splits;
+  const float* p = a.part + (int64_t)(on ? lane : 0) * (4 + 2 * a.k) * a.n + row;
+  const float m = on ? p[0] : -FLT_MAX;
+  float mm = m;
+  for (int off = 32; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor(mm, off, 64));
+  const float dy = fmaxf((m - mm) * a.c2, -1500.0f), f = exp2_hw(dy);
+  float s = on ? p[a.n] : 0.0f;
+  float t = on ? f * fmaf(s, dy, p[2 * a.n]) : 0.0f;
+  int before = on ? __float_as_int(p[3 * a.n]) : 0;
+  s *= f;
+  for (int off = 32; off > 0; off >>= 1) {
+    s += __shfl_xor(s, off, 64);
+    t += __shfl_xor(t, off, 64);
+    before += __shfl_xor(before, off, 64);
+  }
+  const RowStats st{mm, s, t};
+  const int y = a.labels ? a.labels[row] : -1;
+  if (lane == 0) {
+    const float ay = y >= 0 && y < a.d ? static_cast<const float*>(a.F)[(int64_t)y * a.ld + row] : 0.0f;
+    store_row(a, row, st, y, ay, before);
+  }
+  const float ls = st.log_s();
+  int at = 0;  // the lane's place in its split's list
+  for (int q = 0; q < a.k; ++q) {
+    const bool more = on && at < a.k;
+    float v = more ? p[(int64_t)(4 + at) * a.n] : -INFINITY;
+    int id = more ? __float_as_int(p[(int64_t)(4 + a.k + at) * a.n]) : -1;
+    const int mine = id;
+    for (int off = 32; off > 0; off >>= 1) {
+      const float ov = __shfl_xor(v, off, 64);
+      const int oi = __shfl_xor(id, off, 64);
+      if (oi >= 0 && (id < 0 || ov > v || (ov == v && oi < id))) {
+        v = ov;
+        id = oi;
+      }
+    }
+    if (lane == 0) store_top(a, row, q, v, id, st, ls);
+    if (id >= 0 && mine == id) ++at;
+  }
+}
+
+// ---------------------------------------------------------------- a row in a wave's or a block's registers
+// NT threads per row, E elements each; ROWS rows per block.
+constexpr int CAND_WAVE = 256, CAND_BLOCK = 1024;  // places for collected scores
+
+__device__ inline bool better(float v, int j, float ov, int oj) { return v > ov || (v == ov && j < oj); }
+
+// What the threads of one row share.
+template <int NT>
+struct RowShared {
+  static constexpr int W = NT / 64, CAP = NT == 64 ? CAND_WAVE : CAND_BLOCK;
+  float lane_max[W][64];
+  float sums[3][W];
+  float best_v[W];
+  int best_j[W];
+  float cand_v[CAP];
+  int cand_j[CAP];
+  int count;
+  float bound;
+};
+
+template <typename T, int NT, int E>
+__device__ __forceinline__ void row_in_block(const LogProbArgs& a, RowShared<NT>& sh, int64_t row) {
+  constexpr int VEC = 16 / sizeof(T), NV = E / VEC, W = NT / 64, CAP = RowShared<NT>::CAP;
+  const int tid = threadIdx.x & (NT - 1), lane = tid & 63, w = tid >> 6;
+  auto sync = [&]() {
+    if (NT == 64) wave_sync();
+    else __syncthreads();
+  };
+  const T* F = static_cast<const T*>(a.F) + row * a.ld;
+  const int y = a.labels ? a.labels[row] : -1;
+  const float ay = y >= 0 && y < a.d ? to_f32(F[y]) : 0.0f;
+  float x[E];
+#pragma unroll
+  for (int q = 0; q < NV; ++q) {
+    const int j = (q * NT + tid) * VEC;
+    T e[VEC];
+    if (j + VEC <= a.d) {
+      __builtin_memcpy(e, F + j, 16);
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) x[q * VEC + u] = to_f32(e[u]);
+    } else {
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) x[q * VEC + u] = j + u < a.d ? to_f32(F[j + u]) : -INFINITY;
+    }
+  }
+  if (tid == 0) sh.count = 0;
+  float lm = -INFINITY;
+#pragma unroll
+  for (int i = 0; i < E; ++i) lm = fmaxf(lm, x[i]);
+  if (W > 1) {
+    sh.lane_max[w][lane] = lm;
+    sync();
+#pragma unroll
+    for (int u = 0; u < W; ++u) lm = fmaxf(lm, sh.lane_max[u][lane]);
+  }
+  float m = fmaxf(lm, -FLT_MAX);
+  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
   float s = 0.0f, t = 0.0f;
   int before = 0;
-  for (int j = lane; j < a.d; j += 64) {
-    const float v = to_f32(x[j * a.cs]);
-    const float u = (v - mm) * a.c, e = expf(u);
+#pragma unroll
+  for (int i = 0; i < E; ++i) {
+    const float yv = (x[i] - m) * a.c2, e = exp2_hw(yv);
     s += e;
-    t += e * fmaxf(u, -1000.0f);
-    before += v > ay || (v == ay && j < y);
+    t = fmaf(e, fmaxf(yv, -1500.0f), t);
+  }
+  if (a.rank) {
+#pragma unroll
+    for (int q = 0; q < NV; ++q)
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) {
+        const float v = x[q * VEC + u];
+        before += v > ay || (v == ay && (q * NT + tid) * VEC + u < y);
+      }
   }
   for (int off = 32; off > 0; off >>= 1) {
     s += __shfl_xor(s, off, 64);
     t += __shfl_xor(t, off, 64);
     before += __shfl_xor(before, off, 64);
   }
-  const float log_s = logf(s);
-  const bool none = m == -INFINITY && s == 0.0f;
-  if (lane == 0) {
-    if (a.lse) a.lse[row] = mm * a.c + log_s;
-    if (a.entropy) a.entropy[row] = none ? 0.0f : log_s - t / s;
-    if (a.logp) a.logp[row] = !has ? 0.0f : none ? -INFINITY : (ay - mm) * a.c - log_s;
-    if (a.rank) a.rank[row] = has ? before : -1;
+  if (W > 1 && lane == 0) {
+    sh.sums[0][w] = s;
+    sh.sums[1][w] = t;
+    sh.sums[2][w] = __int_as_float(before);
   }
+  if (a.k > 0 && w == 0) {
+    // the k-th largest of the 64 lane maxima: the smallest that fewer than k others exceed
+    int above = 0;
+#pragma unroll
+    for (int l = 0; l < 64; ++l) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lm), l)) > lm;
+    float b = above < a.k ? lm : INFINITY;
+    for (int off = 32; off > 0; off >>= 1) b = fminf(b, __shfl_xor(b, off, 64));
+    if (lane == 0) sh.bound = b;
+  }
+  sync();
+  if (W > 1) {
+    s = t = 0.0f;
+    before = 0;
+#pragma unroll
+    for (int u = 0; u < W; ++u) {
+      s += sh.sums[0][u];
+      t += sh.sums[1][u];
+      before += __float_as_int(sh.sums[2][u]);
+    }
+  }
+  const RowStats st{m, s, t};
+  if (tid == 0) store_row(a, row, st, y, ay, before);
+  if (a.k == 0) return;
+  const float b = sh.bound;
+#pragma unroll
+  for (int q = 0; q < NV; ++q)
+#pragma unroll
+    for (int u = 0; u < VEC; ++u) {
+      const float v = x[q * VEC + u];
+      if (v >= b && v > -INFINITY) {
+        const int at = atomicAdd(&sh.count, 1);
+        if (at < CAP) {
+          sh.cand_v[at] = v;
+          sh.cand_j[at] = (q * NT + tid) * VEC + u;
+        }
+      }
+    }
+  sync();
+  const int found = sh.count;
+  const float ls = st.log_s();
+  if (found <= CAP) {
+    // a score's place is the number of better ones
+    for (int i = tid; i < found; i += NT) {
+      const float v = sh.cand_v[i];
+      const int j = sh.cand_j[i];
+      int place = 0;
+      for (int o = 0; o < found; ++o) place += better(sh.cand_v[o], sh.cand_j[o], v, j);
+      if (place < a.k) store_top(a, row, place, v, j, st, ls);
+    }
+    for (int q = found + tid; q < a.k; q += NT) store_top(a, row, q, -INFINITY, -1, st, ls);
+    return;
+  }
+  // too many (equal scores, or a lane that holds most of the large ones): one
+  // alternative at a time, the best after the one before
   float pv = INFINITY;
   int pj = -1;
-  bool first = true;
   for (int q = 0; q < a.k; ++q) {
-    float bv = -INFINITY;
-    int bj = -1;
-    for (int j = lane; j < a.d; j += 64) {
-      const float v = to_f32(x[j * a.cs]);
-      const bool after = first || v < pv || (v == pv && j > pj);
-      if (after && v > bv) {
-        bv = v;
-        bj = j;
+    float v = -INFINITY;
+    int j = INT_MAX;
+#pragma unroll
+    for (int i = 0; i < NV; ++i)
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) {
+        const float xv = x[i * VEC + u];
+        const int xj = (i * NT + tid) * VEC + u;
+        if (better(pv, pj, xv, xj) && better(xv, xj, v, j)) {
+          v = xv;
+          j = xj;
+        }
       }
-    }
     for (int off = 32; off > 0; off >>= 1) {
-      const float ov = __shfl_xor(bv, off, 64);
-      const int oj = __shfl_xor(bj, off, 64);
-      if (oj >= 0 && (bj < 0 || ov > bv || (ov == bv && oj < bj))) {
-        bv = ov;
-        bj = oj;
+      const float ov = __shfl_xor(v, off, 64);
+      const int oj = __shfl_xor(j, off, 64);
+      if (better(ov, oj, v, j)) {
+        v = ov;
+        j = oj;
       }
     }
-    if (lane == 0) {
-      a.top_id[q * a.ld_top + row] = bj;
-      a.top_logp[q * a.ld_top + row] = bj < 0 ? -INFINITY : (bv - mm) * a.c - log_s;
+    if (W > 1) {
+      __syncthreads();  // the places of the round before are read
+      if (lane == 0) {
+        sh.best_v[w] = v;
+        sh.best_j[w] = j;
+      }
+      __syncthreads();
+#pragma unroll
+      for (int u = 0; u < W; ++u)
+        if (better(sh.best_v[u], sh.best_j[u], v, j)) {
+          v = sh.best_v[u];
+          j = sh.best_j[u];
+        }
     }
-    pv = bj < 0 ? -INFINITY : bv;
-    pj = bj < 0 ? a.d : bj;
-    first = false;
+    if (tid == 0) store_top(a, row, q, v, v > -INFINITY ? j : -1, st, ls);
+    pv = v;
+    pj = j;
   }
+}
+
+// A row of NT threads; a block of 256 has four rows of a wave each.
+template <typename T, int NT, int E>
+__global__ void __launch_bounds__(NT == 64 ? 256 : NT) k_row_in_block(LogProbArgs a) {
+  constexpr int ROWS = NT == 64 ? 4 : 1;
+  __shared__ RowShared<NT> sh[ROWS];
+  const int rg = NT == 64 ? (int)(threadIdx.x >> 6) : 0;
+  for (int64_t row = (int64_t)blockIdx.x * ROWS + rg; row < a.n; row += (int64_t)gridDim.x * ROWS) {
+    row_in_block<T, NT, E>(a, sh[rg], row);
+    if (NT == 64) wave_sync();  // what is shared is read before the next row's
+    else __syncthreads();
+  }
+}
+
+// ---------------------------------------------------------------- launch
+constexpr int MAX_SPLITS = 64;    // lanes of k_join
+constexpr int64_t MAX_BLOCKS = 1 << 20;  // a launch has fewer than 2^32 threads
+constexpr int WANT_WAVES = 2048;  // waves that fill the card: eight per CU
+
+// Column-major scores of few rows: column splits of at least 64 columns and four lists' lengths.
+int column_splits(int64_t n, int32_t d, int32_t k) {
+  const int64_t tiles = (n + 63) / 64;
+  const int least = 4 * k > 64 ? 4 * k : 64;
+  int64_t s = tiles >= WANT_WAVES ? 1 : WANT_WAVES / tiles;
+  if (s > d / least) s = d / least;
+  if (s > MAX_SPLITS) s = MAX_SPLITS;
+  return s < 1 ? 1 : (int)s;
+}
+
+template <template <int> class Launch, typename... Args>
+void by_list(int k, Args... args) {
+  if (k == 0) Launch<0>::run(args...);
+  else if (k == 1) Launch<1>::run(args...);
+  else if (k <= 4) Launch<4>::run(args...);
+  else if (k <= 8) Launch<8>::run(args...);
+  else if (k <= 12) Launch<12>::run(args...);
+  else if (k <= 16) Launch<16>::run(args...);
+  else if (k <= 24) Launch<24>::run(args...);
+  else if (k <= 32) Launch<32>::run(args...);
+  else if (k <= 48) Launch<48>::run(args...);
+  else Launch<64>::run(args...);
+}
+template <int KM>
+struct ColsByLane {
+  static void run(LogProbArgs a, dim3 blocks, hipStream_t st) {
+    hipLaunchKernelGGL(k_cols_by_lane<KM>, blocks, dim3(256), 0, st, a);
+  }
+};
+template <typename T>
+struct RowsByLane {
+  template <int KM>
+  struct With {
+    static void run(LogProbArgs a, dim3 blocks, hipStream_t st) {
+      hipLaunchKernelGGL((k_rows_by_lane<T, KM>), blocks, dim3(256), 0, st, a);
+    }
+  };
+};
+
+template <typename T>
+void launch_rows(LogProbArgs a, hipStream_t st) {
+  // a lane per row where there are rows for the lanes of the card, or few columns for the lanes of a wave
+  if (a.d <= 64 || (a.n >= 32768 && a.d <= 2048)) {
+    by_list<RowsByLane<T>::template With>(a.k, a, dim3((a.tiles + 3) / 4), st);
+    return;
+  }
+  auto blocks = [](int64_t b) { return dim3((unsigned)(b < MAX_BLOCKS ? b : MAX_BLOCKS)); };
+  if (a.d <= 1024) hipLaunchKernelGGL((k_row_in_block<T, 64, 16>), blocks((a.n + 3) / 4), dim3(256), 0, st, a);
+  else if (a.d <= 8192) hipLaunchKernelGGL((k_row_in_block<T, 256, 32>), blocks(a.n), dim3(256), 0, st, a);
+  else hipLaunchKernelGGL((k_row_in_block<T, 1024, 64>), blocks(a.n), dim3(1024), 0, st, a);
 }
 
 }  // namespace
 
-int64_t log_probs_ws_bytes(int64_t, int32_t, int32_t) { return 0; }
+// Workspace: the column splits' statistics and lists.
+int64_t log_probs_ws_bytes(int64_t n, int32_t d, int32_t k) {
+  const int s = column_splits(n, d, k);
+  return s == 1 ? 0 : align256((int64_t)s * (4 + 2 * k) * n * 4);
+}
 
 int32_t launch_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f, double T,
                          const int32_t* labels, float* logp, int32_t* rank, float* lse, float* entropy, int32_t k,
-                         int32_t* top_id, float* top_logp, int64_t ld_top, void*, hipStream_t st) {
-  const bool col = order == SB_COLUMN_MAJOR;
-  const LogProbArgs a{F,    n,   d,       col ? 1 : ld_f, col ? ld_f : 1, (float)(1.0 / T), labels, logp, rank,
-                      lse,  entropy, k,   top_id,         top_logp,       ld_top};
-  const dim3 blocks((unsigned)((n + 3) / 4)), threads(256);
-  if (dtype == SB_F32) hipLaunchKernelGGL(k_log_probs<float>, blocks, threads, 0, st, a);
-  else if (dtype == SB_F16) hipLaunchKernelGGL(k_log_probs<__half>, blocks, threads, 0, st, a);
-  else hipLaunchKernelGGL(k_log_probs<__hip_bfloat16>, blocks, threads, 0, st, a);
+                         int32_t* top_id, float* top_logp, int64_t ld_top, void* ws, hipStream_t st) {
+  LogProbArgs a{F, n, d, ld_f, (float)(1.0 / T), (float)(1.4426950408889634 / T), labels, logp, rank, lse, entropy, k,
+                top_id, top_logp, ld_top, (int)((n + 63) / 64), 1, d, nullptr};
+  if (order == SB_COLUMN_MAJOR && n == 1 && ld_f == 1) {  // one row without gaps is a row-major row
+    order = SB_ROW_MAJOR;
+    a.ld = d;
+  }
+  if (order == SB_COLUMN_MAJOR) {
+    a.splits = column_splits(n, d, k);
+    a.per = (d + a.splits - 1) / a.splits;
+    a.part = static_cast<float*>(ws);
+    const int64_t units = (int64_t)a.tiles * a.splits;
+    by_list<ColsByLane>(k, a, dim3((unsigned)((units + 3) / 4)), st);
+    if (a.splits > 1) hipLaunchKernelGGL(k_join, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, a);
+  } else if (dtype == SB_F32) {
+    launch_rows<float>(a, st);
+  } else if (dtype == SB_F16) {
+    launch_rows<__half>(a, st);
+  } else {
+    launch_rows<__hip_bfloat16>(a, st);
+  }
   return check_launch("sb_log_probs");
 }
 
