@@ -29,7 +29,7 @@
 namespace sb {
 namespace {
 
-constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.693147180559945309f;
+constexpr float LN2 = 0.693147180559945309f;
 
 struct LogProbArgs {
   const void* F;
@@ -54,6 +54,20 @@ __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 __device__ inline float to_f32(float x) { return x; }
 __device__ inline float to_f32(__half x) { return __half2float(x); }
 __device__ inline float to_f32(__hip_bfloat16 x) { return __bfloat162float(x); }
+// The scores in 16 bytes, and 16 bytes of excluded ones.  The compiler sees the bytes
+// anew: it would otherwise widen once and keep both forms.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <typename T>
+__device__ inline void decode(u32x4& raw, float (&x)[16 / sizeof(T)]) {
+  asm volatile("" : "+v"(raw));
+  T e[16 / sizeof(T)];
+  __builtin_memcpy(e, &raw, 16);
+#pragma unroll
+  for (int u = 0; u < (int)(16 / sizeof(T)); ++u) x[u] = to_f32(e[u]);
+}
+__device__ inline uint32_t excluded(float) { return 0xff800000u; }
+__device__ inline uint32_t excluded(__half) { return 0xfc00fc00u; }
+__device__ inline uint32_t excluded(__hip_bfloat16) { return 0xff80ff80u; }
 
 __device__ inline void wave_sync() {
   asm volatile("" ::: "memory");
@@ -132,6 +146,7 @@ struct LaneRow {
       const float yv = (x[i] - mn) * a.c2, e = exp2_hw(yv);
       as += e;
       at = fmaf(e, fmaxf(yv, -1500.0f), at);
+      if (i % 4 == 3) asm volatile("" : "+v"(as), "+v"(at));  // here and now: put off, the terms take registers
     }
     t = fmaf(f, fmaf(s, dy, t), at);
     s = fmaf(f, s, as);
@@ -337,202 +352,293 @@ __global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
 
 // ---------------------------------------------------------------- a row in a wave's or a block's registers
 // NT threads per row, E elements each; ROWS rows per block.
-constexpr int CAND_WAVE = 256, CAND_BLOCK = 1024;  // places for collected scores
+// Places for collected scores, and half as many for 16-byte pieces of the row.
+constexpr int CAND_WAVE = 256, CAND_BLOCK = 1024;
+// Longest lists bounded by 64 maxima; longer ones by 128 (64 of the smallest maxima
+// would let several hundred scores through).
+constexpr int BOUND_ONE = 32;
 
-__device__ inline bool better(float v, int j, float ov, int oj) { return v > ov || (v == ov && j < oj); }
+// Order-preserving bits of a score (both zeros alike), and back.
+__device__ inline uint32_t score_key(float v) {
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  return b ^ (uint32_t)((int32_t)b >> 31 | 0x80000000);
+}
+__device__ inline float key_score(uint32_t k) { return __uint_as_float(k ^ (~(uint32_t)((int32_t)k >> 31) | 0x80000000)); }
+constexpr uint32_t KEY_EXCLUDED = 0x007fffffu;  // of -inf
 
-// What the threads of one row share.
+// What the threads of one row share.  Candidates are ordered by one 64-bit
+// comparison: the score's key, then the smaller class.
 template <int NT>
 struct RowShared {
   static constexpr int W = NT / 64, CAP = NT == 64 ? CAND_WAVE : CAND_BLOCK;
-  float lane_max[W][64];
+  u32x4 piece[CAP / 2];
+  uint64_t cand[CAP];
+  uint64_t best[SB_MAX_TOP];
+  int piece_at[CAP / 2];
+  float lane_max[2][W][64];
   float sums[3][W];
-  float best_v[W];
-  int best_j[W];
-  float cand_v[CAP];
-  int cand_j[CAP];
-  int count;
-  float bound;
+  int pieces[2], count[2];  // of even and odd rows: one is cleared while the other counts
 };
+__device__ inline uint64_t cand_of(float v, int j) { return (uint64_t)score_key(v) << 32 | (uint32_t)~j; }
+__device__ inline float cand_score(uint64_t c) { return key_score((uint32_t)(c >> 32)); }
+__device__ inline int cand_class(uint64_t c) { return (int)~(uint32_t)c; }
 
+// A key that at least k and not many more of the lanes' keys (one or two each) reach,
+// by bisection over its bits; every lane gets it.
+template <bool TWO>
+__device__ inline uint32_t key_bound(uint32_t k0, uint32_t k1, int k) {
+  uint32_t bound = 0;
+  const int enough = k + (k >> 3);
+  for (uint32_t bit = 0x80000000u; bit; bit >>= 1) {
+    const uint32_t t = bound | bit;
+    int n = __popcll(__ballot(k0 >= t));
+    if (TWO) n += __popcll(__ballot(k1 >= t));
+    if (n >= k) {
+      bound = t;
+      if (n <= enough) break;
+    }
+  }
+  return bound;
+}
+
+// The largest float below v, so that x >= v is x > below(v); NaN below -inf, which
+// nothing is "not above".
+__device__ inline float below(float v) {
+  if (v == -INFINITY) return NAN;
+  const uint32_t b = __float_as_uint(v + 0.0f);
+  if (b == 0) return __uint_as_float(0x80000001u);
+  return __uint_as_float(v > 0.0f ? b - 1 : b + 1);
+}
+
+// put(place, candidate) for the k best of the first `found` candidates: a candidate's
+// place is the number of better ones.
+template <int NT, typename Put>
+__device__ inline void ranked(const RowShared<NT>& sh, int found, int k, int tid, Put put) {
+  for (int i = tid; i < found; i += NT) {
+    const uint64_t mine = sh.cand[i];
+    int place = 0, o = 0;
+    for (; o + 8 <= found; o += 8) {
+      uint64_t c[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) c[u] = sh.cand[o + u];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) place += c[u] > mine;
+    }
+    for (; o < found; ++o) place += sh.cand[o] > mine;
+    if (place < k) put(place, mine);
+  }
+}
+
+// Rows of NT threads, E scores each, one after the other: a row's scores are brought
+// while the row before is summed.
 template <typename T, int NT, int E>
-__device__ __forceinline__ void row_in_block(const LogProbArgs& a, RowShared<NT>& sh, int64_t row) {
+__device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT>& sh, int64_t row, int64_t stride) {
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC, W = NT / 64, CAP = RowShared<NT>::CAP;
-  const int tid = threadIdx.x & (NT - 1), lane = tid & 63, w = tid >> 6;
+  int tid = threadIdx.x & (NT - 1);
+  const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   auto sync = [&]() {
     if (NT == 64) wave_sync();
     else __syncthreads();
   };
-  const T* F = static_cast<const T*>(a.F) + row * a.ld;
-  const int y = a.labels ? a.labels[row] : -1;
-  const float ay = y >= 0 && y < a.d ? to_f32(F[y]) : 0.0f;
-  float x[E];
-#pragma unroll
-  for (int q = 0; q < NV; ++q) {
+  // what is left past the last whole 16 bytes is one score per thread
+  const int whole = a.d & ~(VEC - 1);
+  auto row_at = [&](int64_t r) { return static_cast<const T*>(a.F) + r * a.ld; };
+  auto load_vec = [&](const T* F, int q) {
+    const uint32_t none = excluded(T());
+    u32x4 v = u32x4{none, none, none, none};
     const int j = (q * NT + tid) * VEC;
-    T e[VEC];
-    if (j + VEC <= a.d) {
-      __builtin_memcpy(e, F + j, 16);
-#pragma unroll
-      for (int u = 0; u < VEC; ++u) x[q * VEC + u] = to_f32(e[u]);
-    } else {
-#pragma unroll
-      for (int u = 0; u < VEC; ++u) x[q * VEC + u] = j + u < a.d ? to_f32(F[j + u]) : -INFINITY;
-    }
-  }
-  if (tid == 0) sh.count = 0;
-  float lm = -INFINITY;
-#pragma unroll
-  for (int i = 0; i < E; ++i) lm = fmaxf(lm, x[i]);
-  if (W > 1) {
-    sh.lane_max[w][lane] = lm;
-    sync();
-#pragma unroll
-    for (int u = 0; u < W; ++u) lm = fmaxf(lm, sh.lane_max[u][lane]);
-  }
-  float m = fmaxf(lm, -FLT_MAX);
-  for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
-  float s = 0.0f, t = 0.0f;
-  int before = 0;
-#pragma unroll
-  for (int i = 0; i < E; ++i) {
-    const float yv = (x[i] - m) * a.c2, e = exp2_hw(yv);
-    s += e;
-    t = fmaf(e, fmaxf(yv, -1500.0f), t);
-  }
-  if (a.rank) {
-#pragma unroll
-    for (int q = 0; q < NV; ++q)
-#pragma unroll
-      for (int u = 0; u < VEC; ++u) {
-        const float v = x[q * VEC + u];
-        before += v > ay || (v == ay && (q * NT + tid) * VEC + u < y);
-      }
-  }
-  for (int off = 32; off > 0; off >>= 1) {
-    s += __shfl_xor(s, off, 64);
-    t += __shfl_xor(t, off, 64);
-    before += __shfl_xor(before, off, 64);
-  }
-  if (W > 1 && lane == 0) {
-    sh.sums[0][w] = s;
-    sh.sums[1][w] = t;
-    sh.sums[2][w] = __int_as_float(before);
-  }
-  if (a.k > 0 && w == 0) {
-    // the k-th largest of the 64 lane maxima: the smallest that fewer than k others exceed
-    int above = 0;
-#pragma unroll
-    for (int l = 0; l < 64; ++l) above += __int_as_float(__builtin_amdgcn_readlane(__float_as_int(lm), l)) > lm;
-    float b = above < a.k ? lm : INFINITY;
-    for (int off = 32; off > 0; off >>= 1) b = fminf(b, __shfl_xor(b, off, 64));
-    if (lane == 0) sh.bound = b;
-  }
-  sync();
-  if (W > 1) {
-    s = t = 0.0f;
-    before = 0;
-#pragma unroll
-    for (int u = 0; u < W; ++u) {
-      s += sh.sums[0][u];
-      t += sh.sums[1][u];
-      before += __float_as_int(sh.sums[2][u]);
-    }
-  }
-  const RowStats st{m, s, t};
-  if (tid == 0) store_row(a, row, st, y, ay, before);
-  if (a.k == 0) return;
-  const float b = sh.bound;
+    if (j < whole) __builtin_memcpy(&v, F + j, 16);
+    return v;
+  };
+  // 16-bit scores stay as they are and are widened where they are used
+  u32x4 raw[NV];
+  float tail, ay;
+  int y;
+  auto load_scalars = [&](int64_t r) {
+    const T* F = row_at(r);
+    tail = whole + tid < a.d ? to_f32(F[whole + tid]) : -INFINITY;
+    y = a.labels ? a.labels[r] : -1;
+    ay = y >= 0 && y < a.d ? to_f32(F[y]) : 0.0f;
+  };
 #pragma unroll
   for (int q = 0; q < NV; ++q)
+    if (q * NT * VEC < whole) raw[q] = load_vec(row_at(row), q);
+  load_scalars(row);
+  if (tid == 0) sh.pieces[0] = sh.count[0] = 0;
+  for (int turn = 0; row < a.n; row += stride, turn ^= 1) {
+    // the compiler sees the thread anew in every row: the places of its scores, a
+    // register each, would otherwise be held across the rows
+    asm volatile("" : "+v"(tid));
+    // the maxima of the even vectors and of the odd ones
+    float lm[2] = {tail, -INFINITY};
 #pragma unroll
-    for (int u = 0; u < VEC; ++u) {
-      const float v = x[q * VEC + u];
-      if (v >= b && v > -INFINITY) {
-        const int at = atomicAdd(&sh.count, 1);
-        if (at < CAP) {
-          sh.cand_v[at] = v;
-          sh.cand_j[at] = (q * NT + tid) * VEC + u;
-        }
-      }
-    }
-  sync();
-  const int found = sh.count;
-  const float ls = st.log_s();
-  if (found <= CAP) {
-    // a score's place is the number of better ones
-    for (int i = tid; i < found; i += NT) {
-      const float v = sh.cand_v[i];
-      const int j = sh.cand_j[i];
-      int place = 0;
-      for (int o = 0; o < found; ++o) place += better(sh.cand_v[o], sh.cand_j[o], v, j);
-      if (place < a.k) store_top(a, row, place, v, j, st, ls);
-    }
-    for (int q = found + tid; q < a.k; q += NT) store_top(a, row, q, -INFINITY, -1, st, ls);
-    return;
-  }
-  // too many (equal scores, or a lane that holds most of the large ones): one
-  // alternative at a time, the best after the one before
-  float pv = INFINITY;
-  int pj = -1;
-  for (int q = 0; q < a.k; ++q) {
-    float v = -INFINITY;
-    int j = INT_MAX;
+    for (int q = 0; q < NV; ++q) {
+      if (q * NT * VEC >= whole) continue;
+      float x[VEC];
+      decode<T>(raw[q], x);
 #pragma unroll
-    for (int i = 0; i < NV; ++i)
-#pragma unroll
-      for (int u = 0; u < VEC; ++u) {
-        const float xv = x[i * VEC + u];
-        const int xj = (i * NT + tid) * VEC + u;
-        if (better(pv, pj, xv, xj) && better(xv, xj, v, j)) {
-          v = xv;
-          j = xj;
-        }
-      }
-    for (int off = 32; off > 0; off >>= 1) {
-      const float ov = __shfl_xor(v, off, 64);
-      const int oj = __shfl_xor(j, off, 64);
-      if (better(ov, oj, v, j)) {
-        v = ov;
-        j = oj;
-      }
+      for (int u = 0; u < VEC; ++u) lm[q & 1] = fmaxf(lm[q & 1], x[u]);
+      asm volatile("" : "+v"(lm[q & 1]));
     }
     if (W > 1) {
-      __syncthreads();  // the places of the round before are read
-      if (lane == 0) {
-        sh.best_v[w] = v;
-        sh.best_j[w] = j;
-      }
-      __syncthreads();
-#pragma unroll
-      for (int u = 0; u < W; ++u)
-        if (better(sh.best_v[u], sh.best_j[u], v, j)) {
-          v = sh.best_v[u];
-          j = sh.best_j[u];
-        }
+      sh.lane_max[0][w][lane] = lm[0];
+      sh.lane_max[1][w][lane] = lm[1];
     }
-    if (tid == 0) store_top(a, row, q, v, v > -INFINITY ? j : -1, st, ls);
-    pv = v;
-    pj = j;
+    sync();  // 1
+    if (W > 1) {
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+#pragma unroll
+        for (int u = 0; u < W; ++u) lm[h] = fmaxf(lm[h], sh.lane_max[h][u][lane]);
+    }
+    if (tid == 0) sh.pieces[turn ^ 1] = sh.count[turn ^ 1] = 0;
+    float m = fmaxf(fmaxf(lm[0], lm[1]), -FLT_MAX);
+    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    float b = INFINITY;  // candidates are the scores from here on
+    if (a.k > 0) {
+      const uint32_t kb = a.k > BOUND_ONE ? key_bound<true>(score_key(lm[0]), score_key(lm[1]), a.k)
+                                          : key_bound<false>(score_key(fmaxf(lm[0], lm[1])), 0, a.k);
+      // -inf is no candidate; the lowest score above it is -FLT_MAX
+      b = kb > KEY_EXCLUDED ? key_score(kb) : -FLT_MAX;
+    }
+    float s = 0.0f, t = 0.0f;
+    int before = 0;
+    auto add = [&](float xv) {
+      const float yv = (xv - m) * a.c2, e = exp2_hw(yv);
+      s += e;
+      t = fmaf(e, fmaxf(yv, -1500.0f), t);
+    };
+    auto collect = [&](float xv, int j) {
+      if (xv >= b) {
+        const int at = atomicAdd(&sh.count[turn], 1);
+        if (at < CAP) sh.cand[at] = cand_of(xv, j);
+      }
+    };
+    add(tail);
+    if (a.rank) before = tail > ay || (tail == ay && whole + tid < y);
+    if (a.k > 0) collect(tail, whole + tid);
+    const float ay_below = below(ay);
+    const bool more = row + stride < a.n;
+    const T* next = row_at(more ? row + stride : row);
+#pragma unroll
+    for (int q = 0; q < NV; ++q) {
+      if (q * NT * VEC >= whole) continue;
+      float x[VEC];
+      decode<T>(raw[q], x);
+      const int j = (q * NT + tid) * VEC;
+#pragma unroll
+      for (int u = 0; u < VEC; ++u) add(x[u]);
+      asm volatile("" : "+v"(s), "+v"(t));  // here and now: put off, the terms take more registers than there are
+      if (a.rank) {
+        // classes before y come first at equal scores; y's own vector is all "behind" it, but for its equals
+        const float over = j + VEC <= y ? ay_below : ay;
+#pragma unroll
+        for (int u = 0; u < VEC; ++u) before += !(x[u] <= over);
+        if (j <= y && y < j + VEC) {
+#pragma unroll
+          for (int u = 0; u < VEC; ++u) before += x[u] == ay && j + u < y;
+        }
+        asm volatile("" : "+v"(before));
+      }
+      if (a.k > 0) {
+        float xm = x[0];
+#pragma unroll
+        for (int u = 1; u < VEC; ++u) xm = fmaxf(xm, x[u]);
+        if (xm >= b) {  // the 16 bytes that hold a candidate
+          const int at = atomicAdd(&sh.pieces[turn], 1);
+          if (at < CAP / 2) {
+            sh.piece[at] = raw[q];
+            sh.piece_at[at] = j;
+          }
+        }
+      }
+      if (more) raw[q] = load_vec(next, q);
+    }
+    for (int off = 32; off > 0; off >>= 1) {
+      s += __shfl_xor(s, off, 64);
+      t += __shfl_xor(t, off, 64);
+      before += __shfl_xor(before, off, 64);
+    }
+    if (W > 1 && lane == 0) {
+      sh.sums[0][w] = s;
+      sh.sums[1][w] = t;
+      sh.sums[2][w] = __int_as_float(before);
+    }
+    const int y_now = y;
+    const float ay_now = ay;
+    if (more) load_scalars(row + stride);
+    sync();  // 2
+    if (W > 1) {
+      s = t = 0.0f;
+      before = 0;
+#pragma unroll
+      for (int u = 0; u < W; ++u) {
+        s += sh.sums[0][u];
+        t += sh.sums[1][u];
+        before += __float_as_int(sh.sums[2][u]);
+      }
+    }
+    const RowStats st{m, s, t};
+    if (tid == 0) store_row(a, row, st, y_now, ay_now, before);
+    if (a.k == 0) continue;
+    const int pieces = sh.pieces[turn];
+    for (int i = tid; i < (pieces < CAP / 2 ? pieces : CAP / 2) * VEC; i += NT) {
+      const T* e = reinterpret_cast<const T*>(&sh.piece[i / VEC]);
+      collect(to_f32(e[i % VEC]), sh.piece_at[i / VEC] + i % VEC);
+    }
+    sync();  // 3
+    int found = sh.count[turn];
+    const float ls = st.log_s();
+    if (pieces <= CAP / 2 && found <= CAP) {
+      ranked<NT>(sh, found, a.k, tid,
+                 [&](int place, uint64_t c) { store_top(a, row, place, cand_score(c), cand_class(c), st, ls); });
+    } else {
+      // Too many (equal scores, or lanes that hold most of the large ones): the row once
+      // more, in order, and the k best so far whenever the places run out; from then on a
+      // candidate is above the k-th.
+      constexpr int PART = NT < CAP / 2 ? NT : CAP / 2;
+      const T* F = row_at(row);
+      uint32_t above = score_key(b) - 1;
+      found = 0;
+      for (int j0 = 0; j0 < a.d; j0 += PART) {
+        sync();  // the places are free, and the count is read
+        if (tid == 0) sh.count[turn] = found;
+        sync();
+        const int j = j0 + tid;
+        if (tid < PART && j < a.d) {
+          const float v = to_f32(F[j]);
+          if (v > -INFINITY && score_key(v) > above) sh.cand[atomicAdd(&sh.count[turn], 1)] = cand_of(v, j);
+        }
+        sync();
+        found = sh.count[turn];
+        if (found + PART > CAP || j0 + PART >= a.d) {
+          ranked<NT>(sh, found, a.k, tid, [&](int place, uint64_t c) { sh.best[place] = c; });
+          sync();
+          found = found < a.k ? found : a.k;
+          for (int i = tid; i < found; i += NT) sh.cand[i] = sh.best[i];
+          if (found == a.k) above = (uint32_t)(sh.best[a.k - 1] >> 32);
+        }
+      }
+      sync();
+      for (int i = tid; i < found; i += NT)
+        store_top(a, row, i, cand_score(sh.cand[i]), cand_class(sh.cand[i]), st, ls);
+    }
+    for (int q = found + tid; q < a.k; q += NT) store_top(a, row, q, -INFINITY, -1, st, ls);
   }
 }
 
-// A row of NT threads; a block of 256 has four rows of a wave each.
+// A block of 256 has four rows of a wave each, or one row.
 template <typename T, int NT, int E>
 __global__ void __launch_bounds__(NT == 64 ? 256 : NT) k_row_in_block(LogProbArgs a) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
   __shared__ RowShared<NT> sh[ROWS];
-  const int rg = NT == 64 ? (int)(threadIdx.x >> 6) : 0;
-  for (int64_t row = (int64_t)blockIdx.x * ROWS + rg; row < a.n; row += (int64_t)gridDim.x * ROWS) {
-    row_in_block<T, NT, E>(a, sh[rg], row);
-    if (NT == 64) wave_sync();  // what is shared is read before the next row's
-    else __syncthreads();
-  }
+  const int rg = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+  const int64_t row = (int64_t)blockIdx.x * ROWS + rg;
+  if (row < a.n) rows_in_block<T, NT, E>(a, sh[rg], row, (int64_t)gridDim.x * ROWS);
 }
 
 // ---------------------------------------------------------------- launch
 constexpr int MAX_SPLITS = 64;    // lanes of k_join
-constexpr int64_t MAX_BLOCKS = 1 << 20;  // a launch has fewer than 2^32 threads
 constexpr int WANT_WAVES = 2048;  // waves that fill the card: eight per CU
 
 // Column-major scores of few rows: column splits of at least 64 columns and four lists' lengths.
@@ -581,10 +687,22 @@ void launch_rows(LogProbArgs a, hipStream_t st) {
     by_list<RowsByLane<T>::template With>(a.k, a, dim3((a.tiles + 3) / 4), st);
     return;
   }
-  auto blocks = [](int64_t b) { return dim3((unsigned)(b < MAX_BLOCKS ? b : MAX_BLOCKS)); };
-  if (a.d <= 1024) hipLaunchKernelGGL((k_row_in_block<T, 64, 16>), blocks((a.n + 3) / 4), dim3(256), 0, st, a);
-  else if (a.d <= 8192) hipLaunchKernelGGL((k_row_in_block<T, 256, 32>), blocks(a.n), dim3(256), 0, st, a);
-  else hipLaunchKernelGGL((k_row_in_block<T, 1024, 64>), blocks(a.n), dim3(1024), 0, st, a);
+  // else a wave or a block; few rows take more threads each
+  auto blocks = [](int64_t b, int most = 256 * 8) { return dim3((unsigned)(b < most ? b : most)); };
+  if (a.d <= 1024)
+    hipLaunchKernelGGL((k_row_in_block<T, 64, 16>), blocks((a.n + 3) / 4), dim3(256), 0, st, a);
+  else if (a.d <= 4096 && a.n >= WANT_WAVES)
+    hipLaunchKernelGGL((k_row_in_block<T, 64, 64>), blocks((a.n + 3) / 4), dim3(256), 0, st, a);
+  else if (a.d <= 4096)
+    hipLaunchKernelGGL((k_row_in_block<T, 256, 16>), blocks(a.n), dim3(256), 0, st, a);
+  else if (a.d <= 16384 && a.n >= WANT_WAVES / 4)
+    hipLaunchKernelGGL((k_row_in_block<T, 256, 64>), blocks(a.n, 1024), dim3(256), 0, st, a);
+  else if (a.d <= 16384)
+    hipLaunchKernelGGL((k_row_in_block<T, 1024, 16>), blocks(a.n), dim3(1024), 0, st, a);
+  else if constexpr (sizeof(T) == 2)  // two blocks share a CU: one row's loads meet another's arithmetic
+    hipLaunchKernelGGL((k_row_in_block<T, 512, 128>), blocks(a.n, 512), dim3(512), 0, st, a);
+  else
+    hipLaunchKernelGGL((k_row_in_block<T, 1024, 64>), blocks(a.n, 256), dim3(1024), 0, st, a);
 }
 
 }  // namespace
