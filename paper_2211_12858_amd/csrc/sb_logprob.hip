@@ -101,34 +101,49 @@ __device__ inline void store_top(const LogProbArgs& a, int64_t row, int place, f
 constexpr int CH = 16;         // columns per step
 constexpr int TILE_B = 144;    // bytes of a row's 128 in the LDS tile: lanes' 16-byte reads fall on different banks
 
+// A place of a lane's list as one double: the score, exact in the upper 23 bits of the
+// mantissa, and in the lower ones the class, so that of two equal scores the smaller
+// class is the larger double.  Minima and maxima of doubles then move score and class
+// together, at the rate of 32-bit ones.  Both zeros are +0 here, whose doubles are
+// subnormal; no double of a class rounds to another score.  (+inf, which has no room
+// for a class, counts as the largest finite score.)
+__device__ inline double place_of(float x, int j) {
+  const double v = (double)(fminf(x, FLT_MAX) + 0.0f);
+  const uint32_t low = __double2loint(v) | (x < 0.0f ? (uint32_t)j : 0xffffu - (uint32_t)j);
+  return __hiloint2double(__double2hiint(v), (int)low);
+}
+__device__ inline float place_score(double p) { return (float)p; }
+__device__ inline int place_class(double p) {
+  const int low = __double2loint(p) & 0xffff;
+  return p == -INFINITY ? -1 : p < 0.0 ? low : 0xffff - low;
+}
+// The larger of v and p stays in v, the smaller is returned.
+__device__ inline double keep_larger(double& v, double p) {
+  double r;
+  // in one piece, so that v stays in its registers
+  asm("v_min_f64 %1, %0, %2\n\tv_max_f64 %0, %0, %2" : "+v"(v), "=&v"(r) : "v"(p));
+  return r;
+}
+
 template <int KM>
 struct LaneRow {
   float m = -FLT_MAX, s = 0.0f, t = 0.0f;
   int before = 0;
-  float v[KM ? KM : 1];
-  int id[KM ? KM : 1];
+  float last = INFINITY;  // the list's last score
+  double v[KM ? KM : 1];
 
   // Places past k start at +inf, in front, where nothing gets before them: the
   // list's last place is the k-th.
   __device__ void clear(int k) {
 #pragma unroll
-    for (int q = 0; q < KM; ++q) {
-      v[q] = q < KM - k ? INFINITY : -INFINITY;
-      id[q] = -1;
-    }
+    for (int q = 0; q < KM; ++q) v[q] = q < KM - k ? INFINITY : -INFINITY;
+    if (KM) last = -INFINITY;
   }
-  // x above the last place (or -inf: nothing changes): the places that it beats move on by one.
-  __device__ void insert(float x, int j) {
-    bool c[KM ? KM : 1];
+  // A place between those that it is below and those that it beats, which move on by
+  // one (-inf: nothing changes).
+  __device__ void insert(double p) {
 #pragma unroll
-    for (int q = 0; q < KM; ++q) c[q] = x > v[q];
-#pragma unroll
-    for (int q = KM - 1; q > 0; --q) {
-      v[q] = __builtin_amdgcn_fmed3f(v[q - 1], x, v[q]);
-      id[q] = c[q] ? (c[q - 1] ? id[q - 1] : j) : id[q];
-    }
-    v[0] = fmaxf(v[0], x);
-    id[0] = c[0] ? j : id[0];
+    for (int q = 0; q < KM; ++q) p = keep_larger(v[q], p);
   }
   // Columns j0 .. j0 + CH - 1 (those past the last are -inf); again(i) is column
   // j0 + i once more, for i that differs from lane to lane.
@@ -137,7 +152,7 @@ struct LaneRow {
     float mn = x[0];
 #pragma unroll
     for (int i = 1; i < CH; ++i) mn = fmaxf(mn, x[i]);
-    const bool news = KM > 0 && mn > v[KM ? KM - 1 : 0];
+    const bool news = KM > 0 && mn > last;
     mn = fmaxf(m, mn);
     const float dy = fmaxf((m - mn) * a.c2, -1500.0f), f = exp2_hw(dy);
     float as = 0.0f, at = 0.0f;
@@ -158,16 +173,16 @@ struct LaneRow {
     if (KM > 0 && __any(news)) {
       // a bit per column above the list's last place, the first column highest;
       // then the lanes' columns one after the other
-      const float last = v[KM ? KM - 1 : 0];
       uint32_t bits = 0;
 #pragma unroll
       for (int i = 0; i < CH; ++i) bits = 2 * bits + (x[i] > last);
-      while (__any(bits != 0)) {
+      do {
         const int i = CH - 32 + __builtin_clz(bits | 1);
-        const float xi = bits ? again(i) : -INFINITY;
-        insert(xi, j0 + i);
+        const double p = place_of(again(i), j0 + i);
+        insert(bits ? p : -INFINITY);
         bits &= ~(1u << (CH - 1 - i));
-      }
+      } while (__any(bits != 0));
+      last = place_score(v[KM ? KM - 1 : 0]);
     }
   }
 };
@@ -180,7 +195,7 @@ __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t
     const float ls = st.log_s();
 #pragma unroll
     for (int q = 0; q < KM; ++q)
-      if (q >= KM - a.k) store_top(a, row, q - (KM - a.k), r.v[q], r.id[q], st, ls);
+      if (q >= KM - a.k) store_top(a, row, q - (KM - a.k), place_score(r.v[q]), place_class(r.v[q]), st, ls);
     return;
   }
   float* p = a.part + (int64_t)split * (4 + 2 * a.k) * a.n + row;
@@ -191,8 +206,8 @@ __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t
 #pragma unroll
   for (int q = 0; q < KM; ++q)
     if (q >= KM - a.k) {
-      p[(int64_t)(4 + q - (KM - a.k)) * a.n] = r.v[q];
-      p[(int64_t)(4 + a.k + q - (KM - a.k)) * a.n] = __int_as_float(r.id[q]);
+      p[(int64_t)(4 + q - (KM - a.k)) * a.n] = place_score(r.v[q]);
+      p[(int64_t)(4 + a.k + q - (KM - a.k)) * a.n] = __int_as_float(place_class(r.v[q]));
     }
 }
 
@@ -215,27 +230,35 @@ __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
   const float ay = y >= 0 && y < a.d ? F[(int64_t)y * a.ld + loc] : 0.0f;
   LaneRow<KM> r;
   r.clear(a.k);
-  float x[CH], nx[CH];
+  float* mine = lds[KM ? w : 0] + (KM ? lane * STEP_S : 0);
+  // two sets of registers in turn: one is read while the other is used
+  float x[2][CH];
   auto load = [&](float (&to)[CH], int j) {
+    const float* p = F + (int64_t)j * a.ld;
+    if (j + CH <= j1) {
 #pragma unroll
-    for (int i = 0; i < CH; ++i) {
-      const int col = j + i < j1 ? j + i : j1 - 1;
-      to[i] = (F + (int64_t)col * a.ld)[loc];
+      for (int i = 0; i < CH; ++i, p += a.ld) to[i] = p[loc];
+    } else {
+#pragma unroll
+      for (int i = 0; i < CH; ++i, p += a.ld) {
+        to[i] = -INFINITY;
+        if (j + i < j1) to[i] = p[loc];
+      }
     }
   };
-  load(nx, j0);
-  for (int j = j0; j < j1; j += CH) {
-#pragma unroll
-    for (int i = 0; i < CH; ++i) x[i] = j + i < j1 ? nx[i] : -INFINITY;
-    if (j + CH < j1) load(nx, j + CH);
-    // the lane's own 16 scores, for the few that enter its list
-    float* mine = lds[KM ? w : 0] + (KM ? lane * STEP_S : 0);
-    if (KM) {
+  auto step = [&](float (&now)[CH], float (&next)[CH], int j) {
+    if (j + CH < j1) load(next, j + CH);
+    if (KM) {  // the lane's own scores, for the few that enter its list
 #pragma unroll
       for (int i = 0; i < CH; i += 4)
-        *reinterpret_cast<float4*>(mine + i) = make_float4(x[i], x[i + 1], x[i + 2], x[i + 3]);
+        *reinterpret_cast<float4*>(mine + i) = make_float4(now[i], now[i + 1], now[i + 2], now[i + 3]);
     }
-    r.step(a, x, j, y, ay, [&](int i) { return mine[i]; });
+    r.step(a, now, j, y, ay, [&](int i) { return mine[i]; });
+  };
+  load(x[0], j0);
+  for (int j = j0; j < j1; j += 2 * CH) {
+    step(x[0], x[1], j);
+    if (j + CH < j1) step(x[1], x[0], j + CH);
   }
   if (lane <= left) finish_lane<KM>(a, r, row, split, y, ay);
 }
