@@ -16,9 +16,8 @@
 // registers of a block's waves, lanes on consecutive rows, c columns per lane, so
 // F is read once and every load and store is a run of a column.  Waves exchange
 // maxima and sums in LDS; each handles its share of the tile's list places, and
-// all waves then look through all places for the classes of their own columns: a
-// bit per place in the lane's range, then the set bits write their target into the
-// wave's LDS tile of 16 columns.  The gradients replace the targets in that tile,
+// all waves then look through all places for the classes of their own columns and
+// add their targets to the wave's LDS tile of 16 columns.  The gradients replace the targets in that tile,
 // from which 16 lanes per row segment add the squared column norms in fp64, in a
 // fixed order; a block's sums are one partial.  While a tile's gradients go out
 // the same registers take the next tile's scores.
@@ -59,20 +58,17 @@ __device__ inline void wave_sync() {
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// A list place: class (-1: unused) and value.
+// A list place: class and value; unused ones have class -1 and a value of -inf,
+// whatever they held.
 struct Place {
   int id;
   float v;
 };
 __device__ inline Place load_place(const DistillArgs& a, int t, int64_t row) {
-  Place p;
-  p.id = a.t_id[t * a.ld_t + row];
-  p.v = a.t_val[t * a.ld_t + row];
-  if (p.id < 0 || p.id >= a.d) {  // unused, whatever the value is
-    p.id = -1;
-    p.v = -INFINITY;
-  }
-  return p;
+  return Place{a.t_id[t * a.ld_t + row], a.t_val[t * a.ld_t + row]};
+}
+__device__ inline Place usable(const DistillArgs& a, const Place& p) {
+  return p.id >= 0 && p.id < a.d ? p : Place{-1, -INFINITY};
 }
 
 // The teacher's distribution from the sums over the used places: zs = sum e_t and
@@ -107,13 +103,30 @@ __device__ inline float place_exp(const RowArgs& r, float v, float vmax, float& 
   return e;
 }
 
-// A target of the lane's row into its tile row; seen has a bit per column that holds
-// one already (the tile is zero elsewhere).
-__device__ inline void put_target(float* trow, uint32_t& seen, int c, float v) {
-  const uint32_t bit = 1u << c;
-  if (seen & bit) v += trow[c];
-  trow[c] = v;
-  seen |= bit;
+// The listed places of the tile's rows, class and value or exponential, in LDS.
+struct __align__(8) Listed {
+  int id;
+  float e;
+};
+
+// The targets of the lane's row in its CG columns from jg, added to its (zeroed) tile
+// row.  Only this lane adds there, in the order of the places, so the sums are
+// always the same.  Places are read eight at a time.
+template <int CG, int ROWS>
+__device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, float wt, float* trow) {
+  auto put = [&](const Listed& p) {
+    const uint32_t c = (uint32_t)(p.id - jg);
+    if (c < (uint32_t)CG) __hip_atomic_fetch_add(trow + c, wt * p.e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+  };
+  int s = 0;
+  for (; s + 8 <= K; s += 8) {
+    Listed p[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) p[u] = ent[(s + u) * ROWS + rl];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) put(p[u]);
+  }
+  for (; s < K; ++s) put(ent[s * ROWS + rl]);
 }
 
 // Squared norms of a tile's columns: CG lanes take the columns of a segment's rows,
@@ -135,14 +148,13 @@ __device__ inline double tile_norms(const float* tile, int lane) {
 }
 
 template <int ROWS, int C, int MODE, bool MIX, bool FULLC>
-__device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w, int rg) {
+__device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
   constexpr int PARTS = 64 / ROWS;
   constexpr int CG = C < 16 ? C : 16, S = CG + 4, NG = C / CG;
   const DistillArgs& a = r.a;
   const int W = r.waves, K = a.k;
   const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = PARTS == 1 ? 0 : lane >> 5;
-  float* ent_e = reinterpret_cast<float*>(lds);
-  int* ent_id = reinterpret_cast<int*>(lds) + K * ROWS;
+  Listed* ent = reinterpret_cast<Listed*>(lds);
   float* red = reinterpret_cast<float*>(lds) + 2 * K * ROWS;  // [DISTILL_RED][W][64]
   float* tile = red + DISTILL_RED * W * 64 + w * distill_tile_floats(C);
   float* trow = tile + lane * S;
@@ -190,7 +202,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
 
   int64_t base;
   uint32_t loc;
-  rows_of(blockIdx.x, base, loc);
+  rows_of(bx, base, loc);
   float x[C];
   {
     const float* p = a.F + (int64_t)j0 * a.ld_f + base;
@@ -200,27 +212,32 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       if (STEP && (FULLC || i < last)) p += a.ld_f;
     }
   }
+  // the first places of the wave, and the labels, a tile ahead
+  constexpr int AHEAD = PARTS == 2 ? 2 : 4;
+  const int s0 = w * PARTS + hb;
+  Place ahead[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u)
+    if (s0 + u * W * PARTS < K) ahead[u] = load_place(a, s0 + u * W * PARTS, base + loc);
+  int next_y = a.w > 0.0 ? a.labels[base + loc] : -1;
   double total[NG];
 #pragma unroll
   for (int g = 0; g < NG; ++g) total[g] = 0.0;
 
-  for (int t = blockIdx.x; t < r.tiles; t += gridDim.x) {
+  for (int t = bx; t < r.tiles; t += grid) {
     const int64_t row = base + loc;
     const bool ok = ((int64_t)t * r.groups + rg) * ROWS + rl < a.n;
     // the wave's places: class and value into LDS
     float vm = -INFINITY;
-#pragma unroll 2
-    for (int s = w * PARTS + hb; s < K; s += W * PARTS) {
-      const Place p = load_place(a, s, row);
-      ent_id[s * ROWS + rl] = p.id;
-      ent_e[s * ROWS + rl] = p.v;
+    auto stage = [&](int sl, const Place& p) {
+      ent[sl * ROWS + rl] = Listed{p.id, p.v};
       vm = fmaxf(vm, p.v);
-    }
-    int y = -1;
-    if (a.w > 0.0) {
-      y = a.labels[row];
-      if (y >= a.d) y = -1;
-    }
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u * W * PARTS < K) stage(s0 + u * W * PARTS, usable(a, ahead[u]));
+    for (int sl = s0 + AHEAD * W * PARTS; sl < K; sl += W * PARTS) stage(sl, usable(a, load_place(a, sl, row)));
+    const int y = next_y < a.d ? next_y : -1;
     const float A = y >= 0 ? r.w : 0.0f;
     float m = x[0];
 #pragma unroll
@@ -237,9 +254,9 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       wave_sync();
     }
     float zs = 0.0f, us = 0.0f, s1 = 0.0f, sT = 0.0f;
-    for (int s = w * PARTS + hb; s < K; s += W * PARTS) {
-      const float e = place_exp(r, ent_e[s * ROWS + rl], vm, us);
-      ent_e[s * ROWS + rl] = e;
+    for (int sl = s0; sl < K; sl += W * PARTS) {
+      const float e = place_exp(r, ent[sl * ROWS + rl].e, vm, us);
+      ent[sl * ROWS + rl].e = e;
       zs += e;
     }
     // the compiler sees the last column anew: the tests of columns would otherwise
@@ -284,14 +301,13 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     asm volatile("" : "+v"(m));
     int64_t nbase;
     uint32_t nloc;
-    rows_of(t + gridDim.x < r.tiles ? t + gridDim.x : t, nbase, nloc);
-    // the places of the lane's columns, a bit each
-    uint32_t in_lo = 0, in_hi = 0;
-    for (int s = 0; s < K; ++s) {
-      const bool in = (uint32_t)(ent_id[s * ROWS + rl] - jl) < (uint32_t)C;
-      if (s < 32) in_lo |= in ? 1u << s : 0u;
-      else in_hi |= in ? 1u << (s - 32) : 0u;
-    }
+    rows_of(t + grid < r.tiles ? t + grid : t, nbase, nloc);
+    // the next tile's places and labels, which arrive while this one goes out
+    const int64_t nrow = nbase + nloc;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u * W * PARTS < K) ahead[u] = load_place(a, s0 + u * W * PARTS, nrow);
+    if (a.w > 0.0) next_y = a.labels[nrow];
     float hsum = 0.0f, dot = 0.0f;
     if (MODE == 0) {
       // the loss alone: the scores of the listed classes, through the tile
@@ -300,12 +316,10 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
         wave_sync();
 #pragma unroll
         for (int i = 0; i < CG; ++i) trow[i] = x[g * CG + i];
-        uint64_t left = ((uint64_t)in_hi << 32) | in_lo;
-        while (left) {
-          const int s = __builtin_ctzll(left);
-          left &= left - 1;
-          const uint32_t c = (uint32_t)(ent_id[s * ROWS + rl] - jl - g * CG);
-          if (c < CG) dot += te.wt * ent_e[s * ROWS + rl] * (trow[c] - m);
+        for (int sl = 0; sl < K; ++sl) {
+          const Listed p = ent[sl * ROWS + rl];
+          const uint32_t c = (uint32_t)(p.id - jl - g * CG);
+          if (c < CG) dot += te.wt * p.e * (trow[c] - m);
         }
         const uint32_t cy = (uint32_t)(y - jl - g * CG);
         if (y >= 0 && cy < CG) dot += A * (trow[cy] - m);
@@ -329,16 +343,9 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
         float4* t4 = reinterpret_cast<float4*>(trow);
 #pragma unroll
         for (int q = 0; q < CG / 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        uint32_t seen = 0;
-        uint64_t left = ((uint64_t)in_hi << 32) | in_lo;
-        while (left) {
-          const int s = __builtin_ctzll(left);
-          left &= left - 1;
-          const uint32_t c = (uint32_t)(ent_id[s * ROWS + rl] - jl - g * CG);
-          if (c < CG) put_target(trow, seen, c, te.wt * ent_e[s * ROWS + rl]);
-        }
+        add_targets<CG, ROWS>(ent, K, rl, jl + g * CG, te.wt, trow);
         const uint32_t cy = (uint32_t)(y - jl - g * CG);
-        if (y >= 0 && cy < CG) put_target(trow, seen, cy, A);
+        if (y >= 0 && cy < CG) trow[cy] += A;
 #pragma unroll
         for (int q = 0; q < CG / 4; ++q) {
           const float4 t4v = t4[q];
@@ -426,20 +433,25 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       for (int off = CG; off < 64 / PARTS; off <<= 1) s += __shfl_xor(s, off, 64);
       const int col = jl + g * CG + c;
       if ((lane & (64 / PARTS - 1)) < CG && col < a.d)
-        r.npart[(int64_t)col * r.parts + blockIdx.x * r.groups + rg] = s;
+        r.npart[(int64_t)col * r.parts + bx * r.groups + rg] = s;
     }
   }
 }
 
+// Blocks go to the 8 XCDs in turn; each XCD takes a run of neighbouring tiles, which
+// share cache lines where columns do not start on a line.  The launch has a multiple
+// of 8 blocks.
 template <int ROWS, int C, int MODE, bool MIX>
-__global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs r) {
+__global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs r, int grid) {
   extern __shared__ __align__(16) char smem[];
+  const int bx = (int)(blockIdx.x & 7) * ((grid + 7) >> 3) + (int)(blockIdx.x >> 3);
+  if (bx >= grid) return;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rg = wv / r.waves, w = wv - rg * r.waves;
   const int bytes = 4 * (2 * r.a.k * ROWS + DISTILL_RED * r.waves * 64 + r.waves * distill_tile_floats(C));
   char* lds = smem + rg * bytes;
-  if ((w + 1) * C * (64 / ROWS) <= r.a.d) distill_wave<ROWS, C, MODE, MIX, true>(r, lds, w, rg);
-  else distill_wave<ROWS, C, MODE, MIX, false>(r, lds, w, rg);
+  if ((w + 1) * C * (64 / ROWS) <= r.a.d) distill_wave<ROWS, C, MODE, MIX, true>(r, lds, w, rg, bx, grid);
+  else distill_wave<ROWS, C, MODE, MIX, false>(r, lds, w, rg, bx, grid);
 }
 
 // ---------------------------------------------------------------- wider rows
@@ -510,9 +522,8 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
   const DistillArgs& a = r.a;
   const int K = a.k;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  float* ent_e = reinterpret_cast<float*>(smem);  // [K][64]
-  int* ent_id = reinterpret_cast<int*>(smem) + K * 64;
-  float* tile = ent_e + 2 * K * 64 + w * distill_tile_floats(16);
+  Listed* ent = reinterpret_cast<Listed*>(smem);  // [K][64]
+  float* tile = reinterpret_cast<float*>(smem) + 2 * K * 64 + w * distill_tile_floats(16);
   float* trow = tile + lane * 20;
   const int j0 = blockIdx.x * DISTILL_RANGE + w * WIDE_COLS;
   const int cols = a.d - j0 < WIDE_COLS ? a.d - j0 : WIDE_COLS;  // may be <= 0
@@ -524,9 +535,8 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
     const int64_t row = base + loc;
     float vm = -INFINITY;
     for (int s = w; s < K; s += WIDE_WAVES) {
-      const Place p = load_place(a, s, row);
-      ent_id[s * 64 + lane] = p.id;
-      ent_e[s * 64 + lane] = p.v;
+      const Place p = usable(a, load_place(a, s, row));
+      ent[s * 64 + lane] = Listed{p.id, p.v};
       vm = fmaxf(vm, p.v);
     }
     int y = -1;
@@ -550,8 +560,8 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
     for (int u = 0; u < WIDE_WAVES; ++u) vm = fmaxf(vm, red[0][u][lane]);
     float zs = 0.0f, us = 0.0f;
     for (int s = w; s < K; s += WIDE_WAVES) {
-      const float e = place_exp(r, ent_e[s * 64 + lane], vm, us);
-      ent_e[s * 64 + lane] = e;
+      const float e = place_exp(r, ent[s * 64 + lane].e, vm, us);
+      ent[s * 64 + lane].e = e;
       zs += e;
     }
     red[1][w][lane] = zs;
@@ -573,8 +583,8 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
       // the listed scores, each wave its places
       float dot = 0.0f;
       for (int s = w; s < K; s += WIDE_WAVES) {
-        const int id = ent_id[s * 64 + lane];
-        if (id >= 0) dot += te.wt * ent_e[s * 64 + lane] * (a.F[(int64_t)id * a.ld_f + row] - m);
+        const Listed p = ent[s * 64 + lane];
+        if (p.id >= 0) dot += te.wt * p.e * (a.F[(int64_t)p.id * a.ld_f + row] - m);
       }
       if (w == 0 && y >= 0) dot += A * (a.F[(int64_t)y * a.ld_f + row] - m);
       red[0][w][lane] = dot;  // vm is read before the barrier above
@@ -587,12 +597,6 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
     }
     if (MODE != 0) {
       float hsum = 0.0f;
-      uint32_t in_lo = 0, in_hi = 0;
-      for (int s = 0; s < K; ++s) {
-        const bool in = (uint32_t)(ent_id[s * 64 + lane] - j0) < (uint32_t)WIDE_COLS;
-        if (s < 32) in_lo |= in ? 1u << s : 0u;
-        else in_hi |= in ? 1u << (s - 32) : 0u;
-      }
       for (int c0 = 0; c0 < cols; c0 += 16) {
         const int last = cols - 1 - c0;  // of the group's columns, from its first
         float x[16];
@@ -603,16 +607,9 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
         float4* t4 = reinterpret_cast<float4*>(trow);
 #pragma unroll
         for (int q = 0; q < 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        uint32_t seen = 0;
-        uint64_t left = ((uint64_t)in_hi << 32) | in_lo;
-        while (left) {
-          const int s = __builtin_ctzll(left);
-          left &= left - 1;
-          const uint32_t c = (uint32_t)(ent_id[s * 64 + lane] - j0 - c0);
-          if (c < 16) put_target(trow, seen, c, te.wt * ent_e[s * 64 + lane]);
-        }
+        add_targets<16, 64>(ent, K, lane, j0 + c0, te.wt, trow);
         const uint32_t cy = (uint32_t)(y - j0 - c0);
-        if (y >= 0 && cy < 16) put_target(trow, seen, cy, A);
+        if (y >= 0 && cy < 16) trow[cy] += A;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float4 t4v = t4[q];
@@ -687,9 +684,9 @@ bool in_regs(const DistillArgs& a) {
 
 template <int ROWS, int C, int MODE>
 void launch_regs(const RowArgs& r, const DistillPlan& p, bool mix, hipStream_t st) {
-  const dim3 grid(p.grid), block(64 * p.waves * p.groups);
-  if (mix) hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, true>), grid, block, p.lds, st, r);
-  else hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, false>), grid, block, p.lds, st, r);
+  const dim3 grid((p.grid + 7) / 8 * 8), block(64 * p.waves * p.groups);
+  if (mix) hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, true>), grid, block, p.lds, st, r, p.grid);
+  else hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, false>), grid, block, p.lds, st, r, p.grid);
 }
 
 template <int MODE>

@@ -31,7 +31,8 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
   p.c = d <= 8 ? 8 : d <= 256 ? 16 : 32;
   const int cols = p.c * (64 / p.rows);
   p.waves = (d + cols - 1) / cols;
-  p.groups = p.waves == 1 ? 4 : p.waves == 2 ? 2 : 1;
+  // narrow rows: blocks of four waves, unless there are few tiles for the CUs
+  p.groups = p.waves > 2 || n < 64 * 1024 ? 1 : 4 / p.waves;
   p.lds = p.groups * 4 * (2 * k * p.rows + DISTILL_RED * p.waves * 64 + p.waves * distill_tile_floats(p.c));
   const int64_t rows = (int64_t)p.rows * p.groups;
   p.tiles = (int)((n + rows - 1) / rows);
