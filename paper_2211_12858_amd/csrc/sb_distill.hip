@@ -109,14 +109,20 @@ struct __align__(8) Listed {
   float e;
 };
 
-// The targets of the lane's row in its CG columns from jg, added to its (zeroed) tile
-// row.  Only this lane adds there, in the order of the places, so the sums are
-// always the same.  Places are read eight at a time.
+// The targets of the lane's row in its CG columns from jg, into its (zeroed) tile row:
+// the places' and the label's (class y - jg of weight A).  A class listed again is
+// added to what is there; a bit per column says which are (a float atomic per place
+// instead takes the LDS three clocks a lane).  Places are read eight at a time.
 template <int CG, int ROWS>
-__device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, float wt, float* trow) {
-  auto put = [&](const Listed& p) {
-    const uint32_t c = (uint32_t)(p.id - jg);
-    if (c < (uint32_t)CG) __hip_atomic_fetch_add(trow + c, wt * p.e, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_WAVEFRONT);
+__device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, float wt, int y, float A, float* trow) {
+  uint32_t seen = 0;
+  auto put = [&](uint32_t c, float v) {
+    if (c < (uint32_t)CG) {
+      const uint32_t bit = 1u << c;
+      if (seen & bit) v += trow[c];
+      trow[c] = v;
+      seen |= bit;
+    }
   };
   int s = 0;
   for (; s + 8 <= K; s += 8) {
@@ -124,9 +130,13 @@ __device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, flo
 #pragma unroll
     for (int u = 0; u < 8; ++u) p[u] = ent[(s + u) * ROWS + rl];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) put(p[u]);
+    for (int u = 0; u < 8; ++u) put((uint32_t)(p[u].id - jg), wt * p[u].e);
   }
-  for (; s < K; ++s) put(ent[s * ROWS + rl]);
+  for (; s < K; ++s) {
+    const Listed p = ent[s * ROWS + rl];
+    put((uint32_t)(p.id - jg), wt * p.e);
+  }
+  if (y >= 0) put((uint32_t)(y - jg), A);
 }
 
 // Squared norms of a tile's columns: CG lanes take the columns of a segment's rows,
@@ -343,9 +353,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
         float4* t4 = reinterpret_cast<float4*>(trow);
 #pragma unroll
         for (int q = 0; q < CG / 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        add_targets<CG, ROWS>(ent, K, rl, jl + g * CG, te.wt, trow);
-        const uint32_t cy = (uint32_t)(y - jl - g * CG);
-        if (y >= 0 && cy < CG) trow[cy] += A;
+        add_targets<CG, ROWS>(ent, K, rl, jl + g * CG, te.wt, y, A, trow);
 #pragma unroll
         for (int q = 0; q < CG / 4; ++q) {
           const float4 t4v = t4[q];
@@ -607,9 +615,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
         float4* t4 = reinterpret_cast<float4*>(trow);
 #pragma unroll
         for (int q = 0; q < 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        add_targets<16, 64>(ent, K, lane, j0 + c0, te.wt, trow);
-        const uint32_t cy = (uint32_t)(y - j0 - c0);
-        if (y >= 0 && cy < 16) trow[cy] += A;
+        add_targets<16, 64>(ent, K, lane, j0 + c0, te.wt, y, A, trow);
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
           const float4 t4v = t4[q];
