@@ -163,7 +163,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
   constexpr int CG = C < 16 ? C : 16, S = CG + 4, NG = C / CG;
   const DistillArgs& a = r.a;
   const int W = r.waves, K = a.k;
-  const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = PARTS == 1 ? 0 : lane >> 5;
+  const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = lane / ROWS;
   Listed* ent = reinterpret_cast<Listed*>(lds);
   float* red = reinterpret_cast<float*>(lds) + 2 * K * ROWS;  // [DISTILL_RED][W][64]
   float* tile = red + DISTILL_RED * W * 64 + w * distill_tile_floats(C);
@@ -207,8 +207,17 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     for (int u = 1; u < W; ++u) v += red[(q * W + u) * 64 + lane];
     return v;
   };
-  auto half_sum = [&](float v) { return PARTS == 1 ? v : v + __shfl_xor(v, 32, 64); };
-  auto half_max = [&](float v) { return PARTS == 1 ? v : fmaxf(v, __shfl_xor(v, 32, 64)); };
+  // over the lanes of a row
+  auto part_sum = [&](float v) {
+#pragma unroll
+    for (int off = 32; off >= ROWS; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+  };
+  auto part_max = [&](float v) {
+#pragma unroll
+    for (int off = 32; off >= ROWS; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+  };
 
   int64_t base;
   uint32_t loc;
@@ -223,7 +232,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     }
   }
   // the first places of the wave, and the labels, a tile ahead
-  constexpr int AHEAD = PARTS == 2 ? 2 : 4;
+  constexpr int AHEAD = PARTS == 1 ? 4 : 2;
   const int s0 = w * PARTS + hb;
   Place ahead[AHEAD];
 #pragma unroll
@@ -252,8 +261,8 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     float m = x[0];
 #pragma unroll
     for (int i = 1; i < C; ++i) m = fmaxf(m, x[i]);
-    m = half_max(m);
-    vm = half_max(vm);
+    m = part_max(m);
+    vm = part_max(vm);
     if (W > 1) {
       red_put(0, m);
       red_put(1, vm);
@@ -283,10 +292,10 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
         s1 += live ? e1 : 0.0f;
       }
     }
-    zs = half_sum(zs);
-    us = half_sum(us);
-    sT = half_sum(sT);
-    if (MIX) s1 = half_sum(s1);
+    zs = part_sum(zs);
+    us = part_sum(us);
+    sT = part_sum(sT);
+    if (MIX) s1 = part_sum(s1);
     if (W > 1) {
       red_put(2, zs);
       red_put(3, us);
@@ -410,8 +419,8 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       }
     }
     if (W > 1 || a.loss || a.h_row) {
-      if (a.loss) dot = half_sum(dot);
-      if (MODE == 2 && a.h_row) hsum = half_sum(hsum);
+      if (a.loss) dot = part_sum(dot);
+      if (MODE == 2 && a.h_row) hsum = part_sum(hsum);
       if (W > 1) {
         if (a.loss) red_put(6, dot);
         if (MODE == 2 && a.h_row) red_put(7, hsum);
@@ -433,7 +442,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     loc = nloc;
   }
   if (MODE != 0 && r.npart) {
-    // the row segments of a column, in order; with two parts the upper segments are the second part's
+    // the row segments of a column, in order
     const int c = lane % CG;
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
@@ -683,7 +692,7 @@ __global__ void __launch_bounds__(256) k_distill_hrow(const float* sums, int ran
 
 bool in_regs(const DistillArgs& a) {
   if (a.d > DISTILL_REGS_MAX_D) return false;
-  if (a.d <= 512) return true;
+  if (a.d <= DISTILL_ONE_PART_D) return true;
   return a.ld_f < DISTILL_PARTS_MAX_LD && (!a.G || a.ld_g < DISTILL_PARTS_MAX_LD) &&
          (!a.hess || a.ld_h < DISTILL_PARTS_MAX_LD);
 }
@@ -725,8 +734,8 @@ int64_t norm_bytes(int64_t n, int32_t d, int32_t k) {
 // Workspace: [norm partials][statistics of the ranges, 3 n each][row sums of the hessians, n per range]
 int64_t distill_ws_bytes(int64_t n, int32_t d, int32_t k) {
   int64_t b = norm_bytes(n, d, k);
-  // narrow rows take the ranges only at leading dimensions of 2^24 and more
-  if (d > 512) b += align256((int64_t)distill_wide_plan(n, d).ranges * 4 * n * 4);
+  // narrower rows never take the ranges
+  if (d > DISTILL_ONE_PART_D) b += align256((int64_t)distill_wide_plan(n, d).ranges * 4 * n * 4);
   return b;
 }
 

@@ -8,13 +8,14 @@ namespace sb {
 
 constexpr int DISTILL_MAX_WAVES = 16;
 constexpr int DISTILL_REGS_MAX_D = 1024;
-// lane offsets of the two-part waves are 32-bit byte offsets of up to 63 columns
+constexpr int DISTILL_ONE_PART_D = 512;
+// where a row has two lanes of a wave, their offsets are 32-bit byte offsets of up to 63 columns
 constexpr int64_t DISTILL_PARTS_MAX_LD = int64_t(1) << 24;
 constexpr int DISTILL_RED = 8;  // per-wave values that a block's waves exchange
 
 // Rows in the registers of a block's waves.
 struct DistillPlan {
-  int rows;    // rows per tile: 64 x c columns per wave, or 32 x 2c past 512 columns
+  int rows;    // rows per tile; a wave takes 64 / rows sets of c columns of each
   int c;       // columns per lane
   int waves;   // waves per row tile
   int groups;  // row tiles per block
@@ -27,8 +28,8 @@ constexpr int distill_tile_floats(int c) { return 64 * ((c < 16 ? c : 16) + 4); 
 
 constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
   DistillPlan p{};
-  p.rows = d <= 512 ? 64 : 32;
-  p.c = d <= 8 ? 8 : d <= 256 ? 16 : 32;
+  p.rows = d <= DISTILL_ONE_PART_D ? 64 : 32;
+  p.c = d <= 8 ? 8 : d <= 64 ? 16 : 32;
   const int cols = p.c * (64 / p.rows);
   p.waves = (d + cols - 1) / cols;
   // narrow rows: blocks of four waves, unless there are few tiles for the CUs
@@ -51,7 +52,7 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
 // Wider rows (and leading dimensions that the lanes' offsets do not cover): the
 // statistics of column ranges first, then the outputs range by range.
 constexpr int DISTILL_RANGE = 512;  // columns per block, 128 per wave
-constexpr int DISTILL_SLOTS = 256;  // row tiles in flight, and norm partials per column at most
+constexpr int DISTILL_SLOTS = 512;  // row tiles in flight, and norm partials per column at most
 
 struct DistillWidePlan {
   int ranges;
