@@ -21,12 +21,14 @@
 // from which 16 lanes per row segment add the squared column norms in fp64, in a
 // fixed order; a block's sums are one partial.  While a tile's gradients go out
 // the same registers take the next tile's scores.
-// k_distill_stats, k_distill_range (wider rows): maxima and sums of 512-column
-// ranges, then the outputs range by range, the list places staged per block.
+// k_distill_stats, k_distill_rows, k_distill_range (wider rows): maxima and sums of
+// column ranges, then every row's statistics, targets and loss, then the outputs range
+// by range.
 //
 // exp(z / T) is 2^(z * log2(e) / T) by the hardware's exponential, which returns 0
 // below 2^-126: probabilities under 2^-126 of the row's largest are 0.
 #include <cmath>
+#include <type_traits>
 
 #include "sb_common.h"
 #include "sb_distill_plan.h"
@@ -43,9 +45,10 @@ struct RowArgs {
   float w, b, bt;   // hard weight, B = (1 - w) T, B T
   double* npart;    // [d][parts] or NULL
   int parts;
-  int waves, groups, tiles;  // k_distill_regs
-  float* stats;              // [ranges][3][n]: k_distill_stats
-  int ranges, slots;
+  int waves, groups, tiles;
+  float* stats;  // [ranges][3][n]: k_distill_stats; later [ranges][n]: k_distill_range
+  float* row;    // [ROW_VALUES + k][n]: k_distill_rows
+  int ranges, cols, slots;
 };
 
 // Other lanes of the wave see this wave's LDS writes; the compiler keeps the order.
@@ -109,34 +112,37 @@ struct __align__(8) Listed {
   float e;
 };
 
-// The targets of the lane's row in its CG columns from jg, into its (zeroed) tile row:
-// the places' and the label's (class y - jg of weight A).  A class listed again is
-// added to what is there; a bit per column says which are (a float atomic per place
-// instead takes the LDS three clocks a lane).  Places are read eight at a time.
+// A target of the lane's row into its (zeroed) tile row of CG columns, where c is one
+// of them.  A class listed again is added to what is there; a bit per column says
+// which are (a float atomic per place instead takes the LDS three clocks a lane).
+template <int CG>
+__device__ inline void put_target(float* trow, uint32_t& seen, uint32_t c, float v) {
+  if (c < (uint32_t)CG) {
+    const uint32_t bit = 1u << c;
+    if (seen & bit) v += trow[c];
+    trow[c] = v;
+    seen |= bit;
+  }
+}
+
+// The targets of the columns from jg: the places', eight read at a time, and the
+// label's (class y, weight A).
 template <int CG, int ROWS>
 __device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, float wt, int y, float A, float* trow) {
   uint32_t seen = 0;
-  auto put = [&](uint32_t c, float v) {
-    if (c < (uint32_t)CG) {
-      const uint32_t bit = 1u << c;
-      if (seen & bit) v += trow[c];
-      trow[c] = v;
-      seen |= bit;
-    }
-  };
   int s = 0;
   for (; s + 8 <= K; s += 8) {
     Listed p[8];
 #pragma unroll
     for (int u = 0; u < 8; ++u) p[u] = ent[(s + u) * ROWS + rl];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) put((uint32_t)(p[u].id - jg), wt * p[u].e);
+    for (int u = 0; u < 8; ++u) put_target<CG>(trow, seen, (uint32_t)(p[u].id - jg), wt * p[u].e);
   }
   for (; s < K; ++s) {
     const Listed p = ent[s * ROWS + rl];
-    put((uint32_t)(p.id - jg), wt * p.e);
+    put_target<CG>(trow, seen, (uint32_t)(p.id - jg), wt * p.e);
   }
-  if (y >= 0) put((uint32_t)(y - jg), A);
+  if (y >= 0) put_target<CG>(trow, seen, (uint32_t)(y - jg), A);
 }
 
 // Squared norms of a tile's columns: CG lanes take the columns of a segment's rows,
@@ -473,41 +479,56 @@ __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs
 
 // ---------------------------------------------------------------- wider rows
 constexpr int WIDE_WAVES = 4;
-constexpr int WIDE_COLS = DISTILL_RANGE / WIDE_WAVES;  // columns per wave
+
+// XCD x takes a run of units (range, row tile or slot), so that neighbouring tiles of a
+// range, which share cache lines where columns do not start on a line, meet in its L2.
+__device__ inline int unit_of(int units) {
+  return (int)(blockIdx.x & 7) * ((units + 7) >> 3) + (int)(blockIdx.x >> 3);
+}
 
 // Maximum and sums of exponentials of a 64-row tile's columns in one range: the
 // waves' running maxima and sums, joined in LDS.
 template <bool MIX>
-__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r) {
+__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, int units) {
   __shared__ float red[3][WIDE_WAVES][64];
   const DistillArgs& a = r.a;
+  const int unit = unit_of(units);
+  if (unit >= units) return;
+  const int range = unit / r.tiles;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int range = blockIdx.y;
-  const int64_t base = (int64_t)blockIdx.x * 64;
+  const int64_t base = (int64_t)(unit - range * r.tiles) * 64;
   const int64_t left = a.n - 1 - base;
   const int loc = lane < left ? lane : (int)left;
-  const int j0 = range * DISTILL_RANGE + w * WIDE_COLS;
-  const int j1 = j0 + WIDE_COLS < a.d ? j0 + WIDE_COLS : a.d;
+  const int per = r.cols / WIDE_WAVES, j0 = range * r.cols + w * per;
+  const int j1 = j0 + per < a.d ? j0 + per : a.d;
   float m = -INFINITY, s1 = 0.0f, sT = 0.0f;
-  for (int j = j0; j < j1; j += 16) {
-    float x[16];
+  // two sets of registers in turn: one is read while the other is summed
+  float x[2][16];
+  auto load = [&](float (&to)[16], int j) {
 #pragma unroll
-    for (int i = 0; i < 16; ++i) x[i] = (a.F + (int64_t)(j + i < j1 ? j + i : j1 - 1) * a.ld_f + base)[loc];
-    float cm = x[0];
+    for (int i = 0; i < 16; ++i) to[i] = (a.F + (int64_t)(j + i < j1 ? j + i : j1 - 1) * a.ld_f + base)[loc];
+  };
+  auto step = [&](const float (&now)[16], float (&next)[16], int j) {
+    if (j + 16 < j1) load(next, j + 16);
+    float mn = m;
 #pragma unroll
-    for (int i = 1; i < 16; ++i) cm = fmaxf(cm, x[i]);
-    const float mn = fmaxf(m, cm);
+    for (int i = 0; i < 16; ++i) mn = fmaxf(mn, now[i]);
     float a1 = 0.0f, aT = 0.0f;
 #pragma unroll
     for (int i = 0; i < 16; ++i) {
-      const float z = x[i] - mn;
-      const bool live = j + i < j1;
+      const float z = now[i] - mn;
+      const bool live = j + i < j1;  // columns past the last repeat it
       aT += live ? exp2_hw(z * r.c2) : 0.0f;
       if (MIX) a1 += live ? exp2_hw(z * LOG2E) : 0.0f;
     }
     sT = fmaf(sT, exp2_hw((m - mn) * r.c2), aT);
     if (MIX) s1 = fmaf(s1, exp2_hw((m - mn) * LOG2E), a1);
     m = mn;
+  };
+  if (j0 < j1) load(x[0], j0);
+  for (int j = j0; j < j1; j += 32) {
+    step(x[0], x[1], j);
+    if (j + 16 < j1) step(x[1], x[0], j + 16);
   }
   red[0][w][lane] = m;
   red[1][w][lane] = sT;
@@ -530,151 +551,230 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r) {
   if (MIX) out[2 * a.n] = s1;
 }
 
-// The outputs of a 64-row tile's columns in one range.  MODE 0 (the loss alone) has
-// one range: listed scores are gathered.
+// What the rows' outputs need besides their scores: the joined statistics, the
+// targets of the listed places and the loss.  64 rows per block, ranges and places
+// shared out among its waves.  In the workspace of n floats each:
+//   row[0] max, row[1] coefficient of 2^(z c2) in g, row[2] of 2^(z log2 e),
+//   row[3] 1 / sT, row[4] 1 / s1, row[5] Q, then the targets of the K places.
+constexpr int ROW_VALUES = 6;
+
+template <bool MIX>
+__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
+  __shared__ float red[6][WIDE_WAVES][64];
+  const DistillArgs& a = r.a;
+  const int K = a.k;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t base = (int64_t)blockIdx.x * 64;
+  const int64_t left = a.n - 1 - base;  // rows past the end are row n - 1 again, whose values they store once more
+  const int64_t row = base + (lane < left ? lane : left);
+  float* targets = r.row + ROW_VALUES * a.n + row;
+  auto sum_of = [&](int q) {
+    float s = red[q][0][lane];
+#pragma unroll
+    for (int u = 1; u < WIDE_WAVES; ++u) s += red[q][u][lane];
+    return s;
+  };
+  auto max_of = [&](int q) {
+    float s = red[q][0][lane];
+#pragma unroll
+    for (int u = 1; u < WIDE_WAVES; ++u) s = fmaxf(s, red[q][u][lane]);
+    return s;
+  };
+  float m = -INFINITY, vm = -INFINITY;
+#pragma unroll 4
+  for (int q = w; q < r.ranges; q += WIDE_WAVES) m = fmaxf(m, r.stats[(int64_t)q * 3 * a.n + row]);
+#pragma unroll 4
+  for (int s = w; s < K; s += WIDE_WAVES) vm = fmaxf(vm, usable(a, load_place(a, s, row)).v);
+  red[0][w][lane] = m;
+  red[1][w][lane] = vm;
+  __syncthreads();
+  m = max_of(0);
+  vm = max_of(1);
+  float sT = 0.0f, s1 = 0.0f, zs = 0.0f, us = 0.0f;
+#pragma unroll 4
+  for (int q = w; q < r.ranges; q += WIDE_WAVES) {
+    const float* st = r.stats + (int64_t)q * 3 * a.n + row;
+    const float z = st[0] - m;
+    sT = fmaf(st[a.n], exp2_hw(z * r.c2), sT);
+    if (MIX) s1 = fmaf(st[2 * a.n], exp2_hw(z * LOG2E), s1);
+  }
+#pragma unroll 4
+  for (int s = w; s < K; s += WIDE_WAVES) zs += place_exp(r, usable(a, load_place(a, s, row)).v, vm, us);
+  red[2][w][lane] = sT;
+  red[3][w][lane] = s1;
+  red[4][w][lane] = zs;
+  red[5][w][lane] = us;
+  __syncthreads();
+  sT = sum_of(2);
+  s1 = MIX ? sum_of(3) : sT;
+  zs = sum_of(4);
+  us = sum_of(5);
+  const Teacher te = teacher_of(r, zs, us);
+  int y = -1;
+  if (a.w > 0.0) {
+    y = a.labels[row];
+    if (y >= a.d) y = -1;
+  }
+  const float A = y >= 0 ? r.w : 0.0f;
+  float dot = 0.0f, unused = 0.0f;
+#pragma unroll 4
+  for (int s = w; s < K; s += WIDE_WAVES) {
+    const Place p = usable(a, load_place(a, s, row));
+    const float t = te.wt * place_exp(r, p.v, vm, unused);
+    if (a.G) targets[s * a.n] = t;
+    if (a.loss && p.id >= 0) dot += t * (a.F[(int64_t)p.id * a.ld_f + row] - m);
+  }
+  if (a.loss) {
+    if (w == 0 && y >= 0) dot += A * (a.F[(int64_t)y * a.ld_f + row] - m);
+    red[0][w][lane] = dot;  // the maxima are read before the barrier above
+    __syncthreads();
+    if (w == 0) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - sum_of(0);
+  }
+  if (w == 0 && a.G) {
+    const float BQ = r.b * te.Q, iT = 1.0f / sT, i1 = 1.0f / s1;
+    float* out = r.row + row;
+    out[0] = m;
+    out[a.n] = (MIX ? BQ : A + BQ) * iT;
+    out[2 * a.n] = A * i1;
+    out[3 * a.n] = iT;
+    out[4 * a.n] = i1;
+    out[5 * a.n] = te.Q;
+  }
+}
+
+// The outputs of a 64-row tile's columns in one range.
 template <int MODE, bool MIX>
-__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r) {
+__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, int units) {
   extern __shared__ __align__(16) char smem[];
-  __shared__ float red[3][WIDE_WAVES][64];
+  __shared__ float red[WIDE_WAVES][64];
   const DistillArgs& a = r.a;
   const int K = a.k;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   Listed* ent = reinterpret_cast<Listed*>(smem);  // [K][64]
   float* tile = reinterpret_cast<float*>(smem) + 2 * K * 64 + w * distill_tile_floats(16);
   float* trow = tile + lane * 20;
-  const int j0 = blockIdx.x * DISTILL_RANGE + w * WIDE_COLS;
-  const int cols = a.d - j0 < WIDE_COLS ? a.d - j0 : WIDE_COLS;  // may be <= 0
-  for (int64_t t = blockIdx.y; t * 64 < a.n; t += gridDim.y) {
+  const int unit = unit_of(units);
+  if (unit >= units) return;
+  const int range = unit / r.slots, slot = unit - range * r.slots;
+  const int per = r.cols / WIDE_WAVES, j0 = range * r.cols + w * per;
+  const int cols = a.d - j0 < per ? a.d - j0 : per;  // may be <= 0
+  for (int64_t t = slot; t < r.tiles; t += r.slots) {
     const int64_t base = t * 64;
     const int64_t left_rows = a.n - 1 - base;
     const int loc = lane < left_rows ? lane : (int)left_rows;
     const bool ok = lane <= left_rows;
     const int64_t row = base + loc;
-    float vm = -INFINITY;
-    for (int s = w; s < K; s += WIDE_WAVES) {
-      const Place p = usable(a, load_place(a, s, row));
-      ent[s * 64 + lane] = Listed{p.id, p.v};
-      vm = fmaxf(vm, p.v);
-    }
+    float nx[16];
+    auto load = [&](int c0) {
+      const int last = cols - 1 - c0;
+#pragma unroll
+      for (int i = 0; i < 16; ++i) nx[i] = (a.F + (int64_t)(j0 + c0 + (i < last ? i : last)) * a.ld_f + base)[loc];
+    };
+    if (cols > 0) load(0);
+#pragma unroll 4
+    for (int s = w; s < K; s += WIDE_WAVES)
+      ent[s * 64 + lane] = Listed{a.t_id[s * a.ld_t + row], r.row[(ROW_VALUES + s) * a.n + row]};
+    const float* rv = r.row + row;
+    const float m = rv[0], kT = rv[a.n], k1 = rv[2 * a.n], iT = rv[3 * a.n], i1 = rv[4 * a.n], Q = rv[5 * a.n];
     int y = -1;
     if (a.w > 0.0) {
       y = a.labels[row];
       if (y >= a.d) y = -1;
     }
     const float A = y >= 0 ? r.w : 0.0f;
-    // the row's statistics from the ranges'
-    float m = -INFINITY, sT = 0.0f, s1 = 0.0f;
-    for (int q = 0; q < r.ranges; ++q) m = fmaxf(m, r.stats[(int64_t)q * 3 * a.n + row]);
-    for (int q = 0; q < r.ranges; ++q) {
-      const float* st = r.stats + (int64_t)q * 3 * a.n + row;
-      const float z = st[0] - m;
-      sT = fmaf(st[a.n], exp2_hw(z * r.c2), sT);
-      if (MIX) s1 = fmaf(st[2 * a.n], exp2_hw(z * LOG2E), s1);
-    }
-    red[0][w][lane] = vm;
+    const float hQ = r.b * Q * r.inv_t;
+    const float hT = MIX ? hQ : A + hQ, h1 = A;
     __syncthreads();
+    float hsum = 0.0f;
+    // the places of the wave's columns, a bit each; every group takes its own out
+    uint64_t mine = 0;
+#pragma unroll 8
+    for (int s = 0; s < K; ++s)
+      mine |= (uint64_t)((uint32_t)(ent[s * 64 + lane].id - j0) < (uint32_t)(cols > 0 ? cols : 0)) << s;
+    // 16 columns from c0; all of them exist (FULL), or those up to `last`
+    auto group = [&](auto full, int c0, int last) {
+      constexpr bool FULL = decltype(full)::value;
+      float x[16];
 #pragma unroll
-    for (int u = 0; u < WIDE_WAVES; ++u) vm = fmaxf(vm, red[0][u][lane]);
-    float zs = 0.0f, us = 0.0f;
-    for (int s = w; s < K; s += WIDE_WAVES) {
-      const float e = place_exp(r, ent[s * 64 + lane].e, vm, us);
-      ent[s * 64 + lane].e = e;
-      zs += e;
-    }
-    red[1][w][lane] = zs;
-    red[2][w][lane] = us;
-    __syncthreads();
-    zs = us = 0.0f;
+      for (int i = 0; i < 16; ++i) x[i] = nx[i];
+      if (c0 + 16 < cols) load(c0 + 16);
+      wave_sync();
+      float4* t4 = reinterpret_cast<float4*>(trow);
 #pragma unroll
-    for (int u = 0; u < WIDE_WAVES; ++u) {
-      zs += red[1][u][lane];
-      us += red[2][u][lane];
-    }
-    if (!MIX) s1 = sT;
-    const Teacher te = teacher_of(r, zs, us);
-    const float BQ = r.b * te.Q;
-    const float iT = 1.0f / sT, i1 = 1.0f / s1;
-    const float kT = (MIX ? BQ : A + BQ) * iT, k1 = A * i1;
-    const float hT = MIX ? BQ * r.inv_t : A + BQ * r.inv_t, h1 = A;
-    if (a.loss && blockIdx.x == 0) {
-      // the listed scores, each wave its places
-      float dot = 0.0f;
-      for (int s = w; s < K; s += WIDE_WAVES) {
+      for (int q = 0; q < 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+      uint32_t seen = 0;
+      uint64_t left = mine;
+      while (left) {
+        const int s = __builtin_ctzll(left);
+        left &= left - 1;
         const Listed p = ent[s * 64 + lane];
-        if (p.id >= 0) dot += te.wt * p.e * (a.F[(int64_t)p.id * a.ld_f + row] - m);
+        const uint32_t c = (uint32_t)(p.id - j0 - c0);
+        if (c < 16) mine &= ~(uint64_t(1) << s);
+        put_target<16>(trow, seen, c, p.e);
       }
-      if (w == 0 && y >= 0) dot += A * (a.F[(int64_t)y * a.ld_f + row] - m);
-      red[0][w][lane] = dot;  // vm is read before the barrier above
-      __syncthreads();
-      if (w == 0) {
-        for (int u = 1; u < WIDE_WAVES; ++u) dot += red[0][u][lane];
-        if (ok) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
-      }
-      __syncthreads();
-    }
-    if (MODE != 0) {
-      float hsum = 0.0f;
-      for (int c0 = 0; c0 < cols; c0 += 16) {
-        const int last = cols - 1 - c0;  // of the group's columns, from its first
-        float x[16];
+      if (y >= 0) put_target<16>(trow, seen, (uint32_t)(y - j0 - c0), A);
+      float* Gc = a.G + (int64_t)(j0 + c0) * a.ld_g + base;
+      float* Hc = MODE == 2 && a.hess ? a.hess + (int64_t)(j0 + c0) * a.ld_h + base : nullptr;
 #pragma unroll
-        for (int i = 0; i < 16; ++i)
-          x[i] = (a.F + (int64_t)(j0 + c0 + (i < last ? i : last)) * a.ld_f + base)[loc];
-        wave_sync();
-        float4* t4 = reinterpret_cast<float4*>(trow);
+      for (int q = 0; q < 4; ++q) {
+        const float4 t4v = t4[q];
+        const float tv[4] = {t4v.x, t4v.y, t4v.z, t4v.w};
+        float gv[4];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) t4[q] = make_float4(0.0f, 0.0f, 0.0f, 0.0f);
-        add_targets<16, 64>(ent, K, lane, j0 + c0, te.wt, y, A, trow);
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float4 t4v = t4[q];
-          const float tv[4] = {t4v.x, t4v.y, t4v.z, t4v.w};
-          float gv[4];
-#pragma unroll
-          for (int u = 0; u < 4; ++u) {
-            const int i = q * 4 + u;
-            const float z = x[i] - m;
-            const float eT = exp2_hw(z * r.c2);
-            float gr = fmaf(kT, eT, -tv[u]);
-            float e1 = 0.0f;
+        for (int u = 0; u < 4; ++u) {
+          const int i = q * 4 + u;
+          const bool live = FULL || i <= last;
+          const float z = x[i] - m;
+          const float eT = exp2_hw(z * r.c2);
+          float gr = fmaf(kT, eT, -tv[u]);
+          float e1 = 0.0f;
+          if (MIX) {
+            e1 = exp2_hw(z * LOG2E);
+            gr = fmaf(k1, e1, gr);
+          }
+          // rows past the end store row n - 1's own values once more
+          if (live) Gc[loc] = gr;
+          Gc += a.ld_g;
+          if (MODE == 2) {
+            const float pT = eT * iT;
+            float h = hT * fmaf(-pT, pT, pT);
             if (MIX) {
-              e1 = exp2_hw(z * LOG2E);
-              gr = fmaf(k1, e1, gr);
+              const float p1 = e1 * i1;
+              h = fmaf(h1, fmaf(-p1, p1, p1), h);
             }
-            if (ok && i <= last) (a.G + (int64_t)(j0 + c0 + i) * a.ld_g + base)[loc] = gr;
-            if (MODE == 2) {
-              const float pT = eT * iT;
-              float h = hT * fmaf(-pT, pT, pT);
-              if (MIX) {
-                const float p1 = e1 * i1;
-                h = fmaf(h1, fmaf(-p1, p1, p1), h);
-              }
-              hsum += i <= last ? h : 0.0f;
-              if (a.hess && ok && i <= last) (a.hess + (int64_t)(j0 + c0 + i) * a.ld_h + base)[loc] = h;
+            hsum += live ? h : 0.0f;
+            if (a.hess) {
+              if (live) Hc[loc] = h;
+              Hc += a.ld_h;
             }
-            gv[u] = ok && i <= last ? gr : 0.0f;
           }
-          t4[q] = make_float4(gv[0], gv[1], gv[2], gv[3]);
+          gv[u] = ok && live ? gr : 0.0f;
         }
-        if (r.npart) {
-          wave_sync();
-          double s = tile_norms<16, 1>(tile, lane);
-          s += __shfl_xor(s, 16, 64);
-          s += __shfl_xor(s, 32, 64);
-          if (lane < 16 && lane <= last) {
-            // the slot belongs to this lane: its first tile writes it, the others add in order
-            double* pp = r.npart + (int64_t)(j0 + c0 + lane) * r.parts + blockIdx.y;
-            *pp = t == blockIdx.y ? s : *pp + s;
-          }
+        t4[q] = make_float4(gv[0], gv[1], gv[2], gv[3]);
+      }
+      if (r.npart) {
+        wave_sync();
+        double s = tile_norms<16, 1>(tile, lane);
+        s += __shfl_xor(s, 16, 64);
+        s += __shfl_xor(s, 32, 64);
+        if (lane < 16 && lane <= last) {
+          // the slot belongs to this lane: its first tile writes it, the others add in order
+          double* pp = r.npart + (int64_t)(j0 + c0 + lane) * r.parts + slot;
+          *pp = t == slot ? s : *pp + s;
         }
       }
-      if (MODE == 2 && a.h_row) {
-        red[0][w][lane] = hsum;
-        __syncthreads();
-        if (w == 0 && ok) {
-          for (int u = 1; u < WIDE_WAVES; ++u) hsum += red[0][u][lane];
-          r.stats[(int64_t)r.ranges * 3 * a.n + (int64_t)blockIdx.x * a.n + row] = hsum;
-        }
+    };
+    for (int c0 = 0; c0 < cols; c0 += 16) {
+      const int last = cols - 1 - c0;
+      if (last >= 15) group(std::true_type(), c0, last);
+      else group(std::false_type(), c0, last);
+    }
+    if (MODE == 2 && a.h_row) {
+      red[w][lane] = hsum;
+      __syncthreads();
+      if (w == 0 && ok) {
+        for (int u = 1; u < WIDE_WAVES; ++u) hsum += red[u][lane];
+        r.stats[(int64_t)range * a.n + row] = hsum;  // the ranges' statistics are read by now
       }
     }
     __syncthreads();  // the places and exchanged values are read before the next tile's
@@ -712,12 +812,19 @@ void launch_mode(const RowArgs& r, const DistillPlan& p, bool mix, hipStream_t s
   else launch_regs<64, 8, MODE>(r, p, mix, st);
 }
 
-template <int MODE>
-void launch_range(const RowArgs& r, const DistillWidePlan& p, bool mix, hipStream_t st) {
-  const dim3 grid(MODE == 0 ? 1 : p.ranges, p.slots), block(64 * WIDE_WAVES);
-  const size_t lds = 4 * (2 * r.a.k * 64 + WIDE_WAVES * distill_tile_floats(16));
-  if (mix) hipLaunchKernelGGL((k_distill_range<MODE, true>), grid, block, lds, st, r);
-  else hipLaunchKernelGGL((k_distill_range<MODE, false>), grid, block, lds, st, r);
+template <int MODE, bool MIX>
+void launch_wide(const RowArgs& r, const DistillWidePlan& p, hipStream_t st) {
+  const dim3 block(64 * WIDE_WAVES);
+  auto blocks = [](int units) { return dim3((units + 7) / 8 * 8); };
+  hipLaunchKernelGGL(k_distill_stats<MIX>, blocks(p.ranges * p.tiles), block, 0, st, r, p.ranges * p.tiles);
+  hipLaunchKernelGGL(k_distill_rows<MIX>, dim3(p.tiles), block, 0, st, r);
+  if constexpr (MODE != 0) {
+    const size_t lds = 4 * (2 * r.a.k * 64 + WIDE_WAVES * distill_tile_floats(16));
+    hipLaunchKernelGGL((k_distill_range<MODE, MIX>), blocks(p.ranges * p.slots), block, lds, st, r, p.ranges * p.slots);
+    if (r.a.h_row)
+      hipLaunchKernelGGL(k_distill_hrow, dim3((unsigned)((r.a.n + 255) / 256)), dim3(256), 0, st, r.stats, p.ranges, r.a.n,
+                         r.a.d, r.a.h_row);
+  }
 }
 
 int64_t norm_bytes(int64_t n, int32_t d, int32_t k) {
@@ -731,11 +838,12 @@ int64_t norm_bytes(int64_t n, int32_t d, int32_t k) {
 
 }  // namespace
 
-// Workspace: [norm partials][statistics of the ranges, 3 n each][row sums of the hessians, n per range]
+// Workspace: [norm partials][rows' values and targets][statistics of the ranges]
 int64_t distill_ws_bytes(int64_t n, int32_t d, int32_t k) {
   int64_t b = norm_bytes(n, d, k);
   // narrower rows never take the ranges
-  if (d > DISTILL_ONE_PART_D) b += align256((int64_t)distill_wide_plan(n, d).ranges * 4 * n * 4);
+  if (d > DISTILL_ONE_PART_D)
+    b += align256((int64_t)(ROW_VALUES + k) * n * 4) + align256((int64_t)distill_wide_plan(n, d).ranges * 3 * n * 4);
   return b;
 }
 
@@ -763,18 +871,16 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
   } else {
     const DistillWidePlan p = distill_wide_plan(a.n, a.d);
     r.ranges = p.ranges;
+    r.cols = p.cols;
+    r.tiles = p.tiles;
     r.slots = p.slots;
     r.parts = p.slots;
-    r.stats = reinterpret_cast<float*>(static_cast<char*>(ws) + norm_bytes(a.n, a.d, a.k));
-    const dim3 grid(p.tiles, p.ranges), block(64 * WIDE_WAVES);
-    if (mix) hipLaunchKernelGGL(k_distill_stats<true>, grid, block, 0, st, r);
-    else hipLaunchKernelGGL(k_distill_stats<false>, grid, block, 0, st, r);
-    if (mode == 0) launch_range<0>(r, p, mix, st);
-    else if (mode == 1) launch_range<1>(r, p, mix, st);
-    else launch_range<2>(r, p, mix, st);
-    if (mode == 2 && a.h_row)
-      hipLaunchKernelGGL(k_distill_hrow, dim3((unsigned)((a.n + 255) / 256)), dim3(256), 0, st,
-                         r.stats + (int64_t)p.ranges * 3 * a.n, p.ranges, a.n, a.d, a.h_row);
+    char* at = static_cast<char*>(ws) + norm_bytes(a.n, a.d, a.k);
+    r.row = reinterpret_cast<float*>(at);
+    r.stats = reinterpret_cast<float*>(at + align256((int64_t)(ROW_VALUES + a.k) * a.n * 4));
+    if (mode == 0) mix ? launch_wide<0, true>(r, p, st) : launch_wide<0, false>(r, p, st);
+    else if (mode == 1) mix ? launch_wide<1, true>(r, p, st) : launch_wide<1, false>(r, p, st);
+    else mix ? launch_wide<2, true>(r, p, st) : launch_wide<2, false>(r, p, st);
   }
   if (a.norm2) launch_norm_final(r.npart, a.d, r.parts, a.norm2, st);
   return check_launch(call);

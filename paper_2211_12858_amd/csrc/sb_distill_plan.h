@@ -51,20 +51,27 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
 
 // Wider rows (and leading dimensions that the lanes' offsets do not cover): the
 // statistics of column ranges first, then the outputs range by range.
-constexpr int DISTILL_RANGE = 512;  // columns per block, 128 per wave
-constexpr int DISTILL_SLOTS = 512;  // row tiles in flight, and norm partials per column at most
+constexpr int DISTILL_RANGE = 1024;    // columns per block at most, a quarter per wave
+constexpr int DISTILL_SLOTS = 512;     // row tiles in flight, and norm partials per column at most
+constexpr int DISTILL_BLOCKS = 1024;   // fewer (tile, range) pairs than that take narrower ranges
 
 struct DistillWidePlan {
   int ranges;
+  int cols;   // columns per range, a multiple of 64
   int tiles;  // of 64 rows
   int slots;
 };
 
 constexpr DistillWidePlan distill_wide_plan(int64_t n, int32_t d) {
   DistillWidePlan p{};
-  p.ranges = (d + DISTILL_RANGE - 1) / DISTILL_RANGE;
   p.tiles = (int)((n + 63) / 64);
   p.slots = p.tiles < DISTILL_SLOTS ? p.tiles : DISTILL_SLOTS;
+  int ranges = (d + DISTILL_RANGE - 1) / DISTILL_RANGE;
+  const int wanted = (DISTILL_BLOCKS + p.tiles - 1) / p.tiles;
+  if (ranges < wanted) ranges = wanted;
+  if (ranges > (d + 127) / 128) ranges = (d + 127) / 128;
+  p.cols = ((d + ranges - 1) / ranges + 63) / 64 * 64;
+  p.ranges = (d + p.cols - 1) / p.cols;
   return p;
 }
 
