@@ -51,7 +51,7 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
 
 // Wider rows (and leading dimensions that the lanes' offsets do not cover): the
 // statistics of column ranges first, then the outputs range by range.
-constexpr int DISTILL_RANGE = 1024;    // columns per block at most, a quarter per wave
+constexpr int DISTILL_RANGE = 512;     // columns per block at most, a quarter per wave
 constexpr int DISTILL_SLOTS = 512;     // row tiles in flight, and norm partials per column at most
 constexpr int DISTILL_BLOCKS = 1024;   // fewer (tile, range) pairs than that take narrower ranges
 

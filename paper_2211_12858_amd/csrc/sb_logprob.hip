@@ -47,7 +47,7 @@ struct LogProbArgs {
   float* top_logp;
   int64_t ld_top;
   int tiles, splits, per;  // k_rows_by_lane: row tiles, column splits, columns per split
-  float* part;             // splits > 1: [split][4 + 2 k][n]: m, s, t, before, scores, classes
+  double* part;            // splits > 1: [split][2 + k][n]: (m, s), (t, before), the list
 };
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
@@ -74,6 +74,38 @@ __device__ inline void wave_sync() {
   __builtin_amdgcn_s_waitcnt(0xc07f);
   __builtin_amdgcn_wave_barrier();
   asm volatile("" ::: "memory");
+}
+
+// Reductions over the lanes of a wave, in registers; every lane gets the result.
+// Within rows of 16 the partner differs in one lane bit (quad permutations, mirrors of
+// half rows and rows), then rows and halves of the wave meet by permlane swaps.
+template <int CTRL>
+__device__ inline uint32_t dpp_u32(uint32_t x) {
+  return (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xf, 0xf, false);
+}
+template <typename Op>
+__device__ inline uint32_t wave_all(uint32_t x, Op op) {
+  x = op(x, dpp_u32<0xb1>(x));   // quad_perm [1, 0, 3, 2]
+  x = op(x, dpp_u32<0x4e>(x));   // quad_perm [2, 3, 0, 1]
+  x = op(x, dpp_u32<0x141>(x));  // row_half_mirror
+  x = op(x, dpp_u32<0x140>(x));  // row_mirror
+  const auto r = __builtin_amdgcn_permlane16_swap(x, x, false, false);
+  x = op(r[0], r[1]);
+  const auto h = __builtin_amdgcn_permlane32_swap(x, x, false, false);
+  return op(h[0], h[1]);
+}
+__device__ inline float wave_sum(float x) {
+  return __uint_as_float(wave_all(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(__uint_as_float(a) + __uint_as_float(b));
+  }));
+}
+__device__ inline float wave_max(float x) {
+  return __uint_as_float(wave_all(__float_as_uint(x), [](uint32_t a, uint32_t b) {
+    return __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  }));
+}
+__device__ inline int wave_sum(int x) {
+  return (int)wave_all((uint32_t)x, [](uint32_t a, uint32_t b) { return a + b; });
 }
 
 // The row's real outputs from its statistics.  m starts at -FLT_MAX, so that a row of
@@ -198,17 +230,12 @@ __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t
       if (q >= KM - a.k) store_top(a, row, q - (KM - a.k), place_score(r.v[q]), place_class(r.v[q]), st, ls);
     return;
   }
-  float* p = a.part + (int64_t)split * (4 + 2 * a.k) * a.n + row;
-  p[0] = r.m;
-  p[a.n] = r.s;
-  p[2 * a.n] = r.t;
-  p[3 * a.n] = __int_as_float(r.before);
+  double* p = a.part + (int64_t)split * (2 + a.k) * a.n + row;
+  reinterpret_cast<float2*>(p)[0] = make_float2(r.m, r.s);
+  reinterpret_cast<float2*>(p)[a.n] = make_float2(r.t, __int_as_float(r.before));
 #pragma unroll
   for (int q = 0; q < KM; ++q)
-    if (q >= KM - a.k) {
-      p[(int64_t)(4 + q - (KM - a.k)) * a.n] = place_score(r.v[q]);
-      p[(int64_t)(4 + a.k + q - (KM - a.k)) * a.n] = __int_as_float(place_class(r.v[q]));
-    }
+    if (q >= KM - a.k) p[(int64_t)(2 + q - (KM - a.k)) * a.n] = r.v[q];
 }
 
 constexpr int STEP_S = CH + 4;  // floats of a row's step in LDS
@@ -327,49 +354,68 @@ __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
   if (lane <= left) finish_lane<KM>(a, r, row, 0, y, ay);
 }
 
-// The splits' statistics and lists of one row joined by one wave, lane per split.
-__global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
-  const int lane = threadIdx.x & 63;
-  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  if (row >= a.n) return;
-  const bool on = lane < a.splits;
-  const float* p = a.part + (int64_t)(on ? lane : 0) * (4 + 2 * a.k) * a.n + row;
-  const float m = on ? p[0] : -FLT_MAX;
-  float mm = m;
-  for (int off = 32; off > 0; off >>= 1) mm = fmaxf(mm, __shfl_xor(mm, off, 64));
-  const float dy = fmaxf((m - mm) * a.c2, -1500.0f), f = exp2_hw(dy);
-  float s = on ? p[a.n] : 0.0f;
-  float t = on ? f * fmaf(s, dy, p[2 * a.n]) : 0.0f;
-  int before = on ? __float_as_int(p[3 * a.n]) : 0;
-  s *= f;
-  for (int off = 32; off > 0; off >>= 1) {
-    s += __shfl_xor(s, off, 64);
-    t += __shfl_xor(t, off, 64);
-    before += __shfl_xor(before, off, 64);
+// The splits' statistics and lists of a row joined by G lanes, lane per split.  Each
+// lane has its list's next place and the one after it in hand; the best of the G next
+// places is the row's next alternative.
+template <int CTRL>
+__device__ inline double dpp_place(double p) {
+  return __hiloint2double((int)dpp_u32<CTRL>((uint32_t)__double2hiint(p)), (int)dpp_u32<CTRL>((uint32_t)__double2loint(p)));
+}
+template <int G, typename T, typename Op>
+__device__ inline T group_all(T x, Op op, T (*dpp[4])(T)) {
+#pragma unroll
+  for (int q = 0; q < (G >= 16 ? 4 : 3); ++q) x = op(x, dpp[q](x));
+  if (G == 64) {
+    x = op(x, __shfl_xor(x, 16, 64));
+    x = op(x, __shfl_xor(x, 32, 64));
   }
+  return x;
+}
+
+template <int G>
+__global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
+  const int lane = threadIdx.x & (G - 1);
+  const int64_t row = ((int64_t)blockIdx.x * 256 + threadIdx.x) / G;
+  if (row >= a.n) return;  // whole groups, which exchange nothing with others
+  float (*fdpp[4])(float) = {
+      [](float x) { return __uint_as_float(dpp_u32<0xb1>(__float_as_uint(x))); },
+      [](float x) { return __uint_as_float(dpp_u32<0x4e>(__float_as_uint(x))); },
+      [](float x) { return __uint_as_float(dpp_u32<0x141>(__float_as_uint(x))); },
+      [](float x) { return __uint_as_float(dpp_u32<0x140>(__float_as_uint(x))); }};
+  int (*idpp[4])(int) = {[](int x) { return (int)dpp_u32<0xb1>((uint32_t)x); }, [](int x) { return (int)dpp_u32<0x4e>((uint32_t)x); },
+                         [](int x) { return (int)dpp_u32<0x141>((uint32_t)x); },
+                         [](int x) { return (int)dpp_u32<0x140>((uint32_t)x); }};
+  double (*ddpp[4])(double) = {dpp_place<0xb1>, dpp_place<0x4e>, dpp_place<0x141>, dpp_place<0x140>};
+  auto add = [](auto x, auto y) { return x + y; };
+  const bool on = lane < a.splits;
+  const double* list = a.part + (int64_t)(on ? lane : 0) * (2 + a.k) * a.n + row;
+  const float2* head = reinterpret_cast<const float2*>(list);  // (m, s), then (t, before)
+  const float2 ms = on ? head[0] : make_float2(-FLT_MAX, 0.0f);
+  const float2 tb = on ? head[a.n] : make_float2(0.0f, 0.0f);
+  const float mm = group_all<G>(ms.x, [](float x, float y) { return fmaxf(x, y); }, fdpp);
+  const float dy = fmaxf((ms.x - mm) * a.c2, -1500.0f), f = exp2_hw(dy);
+  const float s = group_all<G>(f * ms.y, add, fdpp);
+  const float t = group_all<G>(f * fmaf(ms.y, dy, tb.x), add, fdpp);
+  const int before = group_all<G>(__float_as_int(tb.y), add, idpp);
   const RowStats st{mm, s, t};
   const int y = a.labels ? a.labels[row] : -1;
   if (lane == 0) {
     const float ay = y >= 0 && y < a.d ? static_cast<const float*>(a.F)[(int64_t)y * a.ld + row] : 0.0f;
     store_row(a, row, st, y, ay, before);
   }
+  if (a.k == 0) return;
   const float ls = st.log_s();
-  int at = 0;  // the lane's place in its split's list
+  list += 2 * a.n;
+  auto place = [&](int at) { return on && at < a.k ? list[(int64_t)at * a.n] : -INFINITY; };
+  int at = 2;
+  double p = place(0), after = place(1);
   for (int q = 0; q < a.k; ++q) {
-    const bool more = on && at < a.k;
-    float v = more ? p[(int64_t)(4 + at) * a.n] : -INFINITY;
-    int id = more ? __float_as_int(p[(int64_t)(4 + a.k + at) * a.n]) : -1;
-    const int mine = id;
-    for (int off = 32; off > 0; off >>= 1) {
-      const float ov = __shfl_xor(v, off, 64);
-      const int oi = __shfl_xor(id, off, 64);
-      if (oi >= 0 && (id < 0 || ov > v || (ov == v && oi < id))) {
-        v = ov;
-        id = oi;
-      }
+    const double best = group_all<G>(p, [](double x, double y) { return x > y ? x : y; }, ddpp);
+    if (lane == (q & (G - 1))) store_top(a, row, q, place_score(best), place_class(best), st, ls);
+    if (p == best && best > -INFINITY) {  // one lane: places of different classes differ
+      p = after;
+      after = place(at++);
     }
-    if (lane == 0) store_top(a, row, q, v, id, st, ls);
-    if (id >= 0 && mine == id) ++at;
   }
 }
 
@@ -516,7 +562,7 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     }
     if (tid == 0) sh.pieces[turn ^ 1] = sh.count[turn ^ 1] = 0;
     float m = fmaxf(fmaxf(lm[0], lm[1]), -FLT_MAX);
-    for (int off = 32; off > 0; off >>= 1) m = fmaxf(m, __shfl_xor(m, off, 64));
+    m = wave_max(m);
     float b = INFINITY;  // candidates are the scores from here on
     if (a.k > 0) {
       const uint32_t kb = a.k > BOUND_ONE ? key_bound<true>(score_key(lm[0]), score_key(lm[1]), a.k)
@@ -577,11 +623,9 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       }
       if (more) raw[q] = load_vec(next, q);
     }
-    for (int off = 32; off > 0; off >>= 1) {
-      s += __shfl_xor(s, off, 64);
-      t += __shfl_xor(t, off, 64);
-      before += __shfl_xor(before, off, 64);
-    }
+    s = wave_sum(s);
+    t = wave_sum(t);
+    if (a.rank) before = wave_sum(before);
     if (W > 1 && lane == 0) {
       sh.sums[0][w] = s;
       sh.sums[1][w] = t;
@@ -705,8 +749,11 @@ struct RowsByLane {
 
 template <typename T>
 void launch_rows(LogProbArgs a, hipStream_t st) {
-  // a lane per row where there are rows for the lanes of the card, or few columns for the lanes of a wave
-  if (a.d <= 64 || (a.n >= 32768 && a.d <= 2048)) {
+  // A lane per row where there are rows for the lanes of the card: its time is that of
+  // d columns until there are some 100,000 rows, a wave's that of the rows.  (us at
+  // fp32, 5 alternatives, by lane and by wave: 10,000 x 40 12.5 and 11.6, 50,000 x 200 33
+  // and 49, 50,000 x 800 84 and 64, 200,000 x 800 166 and 235; fp16 with 16: 298 and 273.)
+  if (a.n >= (int64_t)160 * a.d && a.d <= 640) {
     by_list<RowsByLane<T>::template With>(a.k, a, dim3((a.tiles + 3) / 4), st);
     return;
   }
@@ -733,7 +780,7 @@ void launch_rows(LogProbArgs a, hipStream_t st) {
 // Workspace: the column splits' statistics and lists.
 int64_t log_probs_ws_bytes(int64_t n, int32_t d, int32_t k) {
   const int s = column_splits(n, d, k);
-  return s == 1 ? 0 : align256((int64_t)s * (4 + 2 * k) * n * 4);
+  return s == 1 ? 0 : align256((int64_t)s * (2 + k) * n * 8);
 }
 
 int32_t launch_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f, double T,
@@ -748,10 +795,13 @@ int32_t launch_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n,
   if (order == SB_COLUMN_MAJOR) {
     a.splits = column_splits(n, d, k);
     a.per = (d + a.splits - 1) / a.splits;
-    a.part = static_cast<float*>(ws);
+    a.part = static_cast<double*>(ws);
     const int64_t units = (int64_t)a.tiles * a.splits;
     by_list<ColsByLane>(k, a, dim3((unsigned)((units + 3) / 4)), st);
-    if (a.splits > 1) hipLaunchKernelGGL(k_join, dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, a);
+    auto blocks = [&](int g) { return dim3((unsigned)((n * g + 255) / 256)); };
+    if (a.splits > 16) hipLaunchKernelGGL(k_join<64>, blocks(64), dim3(256), 0, st, a);
+    else if (a.splits > 8) hipLaunchKernelGGL(k_join<16>, blocks(16), dim3(256), 0, st, a);
+    else if (a.splits > 1) hipLaunchKernelGGL(k_join<8>, blocks(8), dim3(256), 0, st, a);
   } else if (dtype == SB_F32) {
     launch_rows<float>(a, st);
   } else if (dtype == SB_F16) {
