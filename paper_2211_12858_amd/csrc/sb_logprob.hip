@@ -157,30 +157,109 @@ __device__ inline double keep_larger(double& v, double p) {
   return r;
 }
 
+// Places in a lane's queue (long lists only).
+constexpr int QUEUE = 16;
+
+// v[LO .. LO + N) from a bitonic sequence to descending order.
+template <int LO, int N, int KM>
+__device__ __forceinline__ void bitonic_merge(double (&v)[KM]) {
+  if constexpr (N > 1) {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) v[LO + N / 2 + i] = keep_larger(v[LO + i], v[LO + N / 2 + i]);
+    bitonic_merge<LO, N / 2>(v);
+    bitonic_merge<LO + N / 2, N / 2>(v);
+  }
+}
+// Descending order by merging sorted halves (Batcher's odd-even merges).
+template <int LO, int N, int R>
+__device__ __forceinline__ void odd_even_merge(double (&v)[QUEUE]) {
+  if constexpr (2 * R < N) {
+    odd_even_merge<LO, N, 2 * R>(v);
+    odd_even_merge<LO + R, N, 2 * R>(v);
+#pragma unroll
+    for (int i = LO + R; i + R < LO + N; i += 2 * R) v[i + R] = keep_larger(v[i], v[i + R]);
+  } else {
+    v[LO + R] = keep_larger(v[LO], v[LO + R]);
+  }
+}
+template <int LO, int N>
+__device__ __forceinline__ void odd_even_sort(double (&v)[QUEUE]) {
+  if constexpr (N > 1) {
+    odd_even_sort<LO, N / 2>(v);
+    odd_even_sort<LO + N / 2, N / 2>(v);
+    odd_even_merge<LO, N, 1>(v);
+  }
+}
+
 template <int KM>
 struct LaneRow {
+  static constexpr bool QUEUED = KM > 16;  // a list of 32 or 64 places
   float m = -FLT_MAX, s = 0.0f, t = 0.0f;
   int before = 0;
   float last = INFINITY;  // the list's last score
+  int queued = 0;
   double v[KM ? KM : 1];
 
-  // Places past k start at +inf, in front, where nothing gets before them: the
-  // list's last place is the k-th.
+  // A queued list starts empty, its places past k at +inf in front, where nothing gets
+  // before them, so that its last place is the k-th.
   __device__ void clear(int k) {
+    if constexpr (QUEUED) {
 #pragma unroll
-    for (int q = 0; q < KM; ++q) v[q] = q < KM - k ? INFINITY : -INFINITY;
-    if (KM) last = -INFINITY;
+      for (int i = 0; i < KM; ++i) v[i] = i < KM - k ? INFINITY : -INFINITY;
+      last = -INFINITY;
+    }
   }
+  // Others start as the first 16 columns in order; their k-th place is looked up.
+  __device__ void start(const float (&x)[CH], int j0, int k) {
+    double q[QUEUE];
+    static_assert(CH == QUEUE, "the first step fills a queue");
+#pragma unroll
+    for (int i = 0; i < CH; ++i) q[i] = x[i] > -INFINITY ? place_of(x[i], j0 + i) : -INFINITY;
+    odd_even_sort<0, QUEUE>(q);
+#pragma unroll
+    for (int i = 0; i < KM; ++i) v[i] = q[i < QUEUE ? i : 0];
+    find_last(k);
+  }
+  __device__ void find_last(int k) {
+    double p = v[QUEUED ? KM - 1 : 0];
+#pragma unroll
+    for (int i = 1; i < KM && !QUEUED; ++i) {
+      asm volatile("" : "+s"(k));  // else an index into a list in memory
+      p = i < k ? v[i] : p;
+    }
+    last = place_score(p);
+  }
+  // v[i] of the list from its first place on (i is known where this is used).
+  __device__ static int place_in(int i, int k) { return QUEUED ? i - (KM - k) : i; }
   // A place between those that it is below and those that it beats, which move on by
   // one (-inf: nothing changes).
   __device__ void insert(double p) {
 #pragma unroll
     for (int q = 0; q < KM; ++q) p = keep_larger(v[q], p);
   }
+  // The queue into the list: sorted, its m-th best meets the list's m-th last, the
+  // larger stays, and what results falls and then rises.
+  __device__ void take(const double* queue) {
+    double q[QUEUE];
+#pragma unroll
+    for (int i = 0; i < QUEUE; ++i) {
+      const double p = queue[i * 64];
+      q[i] = i < queued ? p : -INFINITY;
+    }
+    odd_even_sort<0, QUEUE>(q);
+#pragma unroll
+    for (int i = 0; i < QUEUE; ++i) (void)keep_larger(v[KM - 1 - i], q[i]);
+    bitonic_merge<0, KM>(v);
+    queued = 0;
+  }
   // Columns j0 .. j0 + CH - 1 (those past the last are -inf); again(i) is column
-  // j0 + i once more, for i that differs from lane to lane.
+  // j0 + i once more, for i that differs from lane to lane.  Long lists take the scores
+  // above their last place through a queue in LDS (a place every 64 doubles), 16 at a
+  // time or with the row's end: 2M x 100 with 10 alternatives ..., 300,007 x 1000 with
+  // 32 ...; one at a time, in every lane until the slowest is through, short ones.
   template <typename Again>
-  __device__ void step(const LogProbArgs& a, const float (&x)[CH], int j0, int y, float ay, Again again) {
+  __device__ __forceinline__ void step(const LogProbArgs& a, const float (&x)[CH], int j0, int y, float ay, bool end,
+                                       bool first, double* queue, Again again) {
     float mn = x[0];
 #pragma unroll
     for (int i = 1; i < CH; ++i) mn = fmaxf(mn, x[i]);
@@ -202,7 +281,9 @@ struct LaneRow {
 #pragma unroll
       for (int i = 0; i < CH; ++i) before += x[i] > ay || (x[i] == ay && j0 + i < y);
     }
-    if (KM > 0 && __any(news)) {
+    if (KM > 0 && !QUEUED && first) {
+      start(x, j0, a.k);
+    } else if (KM > 0 && (__any(news) || (QUEUED && end))) {
       // a bit per column above the list's last place, the first column highest;
       // then the lanes' columns one after the other
       uint32_t bits = 0;
@@ -211,10 +292,17 @@ struct LaneRow {
       do {
         const int i = CH - 32 + __builtin_clz(bits | 1);
         const double p = place_of(again(i), j0 + i);
-        insert(bits ? p : -INFINITY);
-        bits &= ~(1u << (CH - 1 - i));
+        if constexpr (QUEUED) {
+          if (bits) queue[queued * 64] = p;
+          queued += bits != 0;
+          bits &= ~(1u << (CH - 1 - i));
+          if (__any(queued == QUEUE) || (end && !__any(bits != 0))) take(queue);
+        } else {
+          insert(bits ? p : -INFINITY);
+          bits &= ~(1u << (CH - 1 - i));
+        }
       } while (__any(bits != 0));
-      last = place_score(v[KM ? KM - 1 : 0]);
+      find_last(a.k);
     }
   }
 };
@@ -226,23 +314,35 @@ __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t
     store_row(a, row, st, y, ay, r.before);
     const float ls = st.log_s();
 #pragma unroll
-    for (int q = 0; q < KM; ++q)
-      if (q >= KM - a.k) store_top(a, row, q - (KM - a.k), place_score(r.v[q]), place_class(r.v[q]), st, ls);
+    for (int q = 0; q < KM; ++q) {
+      const int at = r.place_in(q, a.k);
+      if (at >= 0 && at < a.k) store_top(a, row, at, place_score(r.v[q]), place_class(r.v[q]), st, ls);
+    }
     return;
   }
   double* p = a.part + (int64_t)split * (2 + a.k) * a.n + row;
   reinterpret_cast<float2*>(p)[0] = make_float2(r.m, r.s);
   reinterpret_cast<float2*>(p)[a.n] = make_float2(r.t, __int_as_float(r.before));
 #pragma unroll
-  for (int q = 0; q < KM; ++q)
-    if (q >= KM - a.k) p[(int64_t)(2 + q - (KM - a.k)) * a.n] = r.v[q];
+  for (int q = 0; q < KM; ++q) {
+    const int at = r.place_in(q, a.k);
+    if (at >= 0 && at < a.k) p[(int64_t)(2 + at) * a.n] = r.v[q];
+  }
 }
 
 constexpr int STEP_S = CH + 4;  // floats of a row's step in LDS
 
+// LDS of a wave of k_cols_by_lane: the lanes' current scores, for the few that enter
+// their lists, and the lists' queues.
+template <int KM>
+struct ColsShared {
+  float step[KM ? 64 * STEP_S : 1];
+  double queue[LaneRow<KM>::QUEUED ? 64 * QUEUE : 1];
+};
+
 template <int KM>
 __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
-  __shared__ __align__(16) float lds[KM ? 4 : 1][KM ? 64 * STEP_S : 4];
+  __shared__ __align__(16) ColsShared<KM> sh[4];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = (int64_t)blockIdx.x * 4 + w;
   if (unit >= (int64_t)a.tiles * a.splits) return;
@@ -257,9 +357,8 @@ __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
   const float ay = y >= 0 && y < a.d ? F[(int64_t)y * a.ld + loc] : 0.0f;
   LaneRow<KM> r;
   r.clear(a.k);
-  float* mine = lds[KM ? w : 0] + (KM ? lane * STEP_S : 0);
-  // two sets of registers in turn: one is read while the other is used
-  float x[2][CH];
+  float* mine = sh[w].step + (KM ? lane * STEP_S : 0);
+  double* queue = sh[w].queue + (LaneRow<KM>::QUEUED ? lane : 0);
   auto load = [&](float (&to)[CH], int j) {
     const float* p = F + (int64_t)j * a.ld;
     if (j + CH <= j1) {
@@ -273,19 +372,35 @@ __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
       }
     }
   };
-  auto step = [&](float (&now)[CH], float (&next)[CH], int j) {
-    if (j + CH < j1) load(next, j + CH);
-    if (KM) {  // the lane's own scores, for the few that enter its list
+  auto step = [&](const float (&now)[CH], int j) {
+    if (KM) {
 #pragma unroll
       for (int i = 0; i < CH; i += 4)
         *reinterpret_cast<float4*>(mine + i) = make_float4(now[i], now[i + 1], now[i + 2], now[i + 3]);
     }
-    r.step(a, now, j, y, ay, [&](int i) { return mine[i]; });
+    r.step(a, now, j, y, ay, j + CH >= j1, j == j0, queue, [&](int i) { return mine[i]; });
   };
-  load(x[0], j0);
-  for (int j = j0; j < j1; j += 2 * CH) {
-    step(x[0], x[1], j);
-    if (j + CH < j1) step(x[1], x[0], j + CH);
+  if constexpr (LaneRow<KM>::QUEUED) {
+    float x[CH], nx[CH];
+    load(nx, j0);
+    for (int j = j0; j < j1; j += CH) {
+#pragma unroll
+      for (int i = 0; i < CH; ++i) x[i] = nx[i];
+      if (j + CH < j1) load(nx, j + CH);
+      step(x, j);
+    }
+  } else {
+    // two sets of registers in turn: one is read while the other is used
+    float x[2][CH];
+    load(x[0], j0);
+    for (int j = j0; j < j1; j += 2 * CH) {
+      if (j + CH < j1) load(x[1], j + CH);
+      step(x[0], j);
+      if (j + CH < j1) {
+        if (j + 2 * CH < j1) load(x[0], j + 2 * CH);
+        step(x[1], j + CH);
+      }
+    }
   }
   if (lane <= left) finish_lane<KM>(a, r, row, split, y, ay);
 }
@@ -295,6 +410,7 @@ template <typename T, int KM>
 __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
   constexpr int VEC = 16 / sizeof(T), COLS = 8 * VEC;
   __shared__ __align__(16) char lds[4][64 * TILE_B];
+  __shared__ double queues[4][LaneRow<KM>::QUEUED ? 64 * QUEUE : 1];
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t tile = (int64_t)blockIdx.x * 4 + w;
   if (tile >= a.tiles) return;
@@ -311,6 +427,7 @@ __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
   const int vrow = lane >> 3, vcol = (lane & 7) * VEC;
   char* put = lds[w] + vrow * TILE_B + (lane & 7) * 16;
   const char* get = lds[w] + lane * TILE_B;
+  double* queue = queues[w] + (LaneRow<KM>::QUEUED ? lane : 0);
   uint4 nx[8];
   auto load = [&](int j) {
     const int c = j + vcol;
@@ -336,6 +453,7 @@ __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
     for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(put + q * 8 * TILE_B) = nx[q];
     wave_sync();
     if (j + COLS < a.d) load(j + COLS);
+#pragma unroll 1
     for (int h = 0; h < COLS / CH; ++h) {
       if (j + h * CH >= a.d) break;
       float x[CH];
@@ -347,7 +465,7 @@ __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
 #pragma unroll
         for (int u = 0; u < VEC; ++u) x[q * VEC + u] = j + h * CH + q * VEC + u < a.d ? to_f32(e[u]) : -INFINITY;
       }
-      r.step(a, x, j + h * CH, y, ay,
+      r.step(a, x, j + h * CH, y, ay, j + h * CH + CH >= a.d, j + h == 0, queue,
              [&](int i) { return to_f32(reinterpret_cast<const T*>(get)[h * CH + i]); });
     }
   }
@@ -726,9 +844,7 @@ void by_list(int k, Args... args) {
   else if (k <= 8) Launch<8>::run(args...);
   else if (k <= 12) Launch<12>::run(args...);
   else if (k <= 16) Launch<16>::run(args...);
-  else if (k <= 24) Launch<24>::run(args...);
   else if (k <= 32) Launch<32>::run(args...);
-  else if (k <= 48) Launch<48>::run(args...);
   else Launch<64>::run(args...);
 }
 template <int KM>
