@@ -255,8 +255,9 @@ struct LaneRow {
   // Columns j0 .. j0 + CH - 1 (those past the last are -inf); again(i) is column
   // j0 + i once more, for i that differs from lane to lane.  Long lists take the scores
   // above their last place through a queue in LDS (a place every 64 doubles), 16 at a
-  // time or with the row's end: 2M x 100 with 10 alternatives ..., 300,007 x 1000 with
-  // 32 ...; one at a time, in every lane until the slowest is through, short ones.
+  // time or with the row's end; short ones take them one at a time, all lanes until the
+  // slowest is through.  (300,007 x 1000 with 32 alternatives 309 us, 399 one at a time;
+  // 2M x 100 with 10 alternatives 346 us, 291 one at a time.)
   template <typename Again>
   __device__ __forceinline__ void step(const LogProbArgs& a, const float (&x)[CH], int j0, int y, float ay, bool end,
                                        bool first, double* queue, Again again) {
@@ -617,7 +618,7 @@ __device__ inline void ranked(const RowShared<NT>& sh, int found, int k, int tid
 }
 
 // Rows of NT threads, E scores each, one after the other: a row's scores are brought
-// while the row before is summed.
+// while the alternatives of the row before are ranked.
 template <typename T, int NT, int E>
 __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT>& sh, int64_t row, int64_t stride) {
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC, W = NT / 64, CAP = RowShared<NT>::CAP;
@@ -705,8 +706,6 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     if (a.rank) before = tail > ay || (tail == ay && whole + tid < y);
     if (a.k > 0) collect(tail, whole + tid);
     const float ay_below = below(ay);
-    const bool more = row + stride < a.n;
-    const T* next = row_at(more ? row + stride : row);
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       if (q * NT * VEC >= whole) continue;
@@ -739,7 +738,17 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
           }
         }
       }
-      if (more) raw[q] = load_vec(next, q);
+    }
+    // the registers are free: the next row's scores are on their way through what
+    // follows (among the sums above, each would be waited for at the next vector)
+    const int y_now = y;
+    const float ay_now = ay;
+    if (row + stride < a.n) {
+      const T* next = row_at(row + stride);
+#pragma unroll
+      for (int q = 0; q < NV; ++q)
+        if (q * NT * VEC < whole) raw[q] = load_vec(next, q);
+      load_scalars(row + stride);
     }
     s = wave_sum(s);
     t = wave_sum(t);
@@ -749,9 +758,6 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       sh.sums[1][w] = t;
       sh.sums[2][w] = __int_as_float(before);
     }
-    const int y_now = y;
-    const float ay_now = ay;
-    if (more) load_scalars(row + stride);
     sync();  // 2
     if (W > 1) {
       s = t = 0.0f;
@@ -826,14 +832,15 @@ __global__ void __launch_bounds__(NT == 64 ? 256 : NT) k_row_in_block(LogProbArg
 constexpr int MAX_SPLITS = 64;    // lanes of k_join
 constexpr int WANT_WAVES = 2048;  // waves that fill the card: eight per CU
 
-// Column-major scores of few rows: column splits of at least 64 columns and four lists' lengths.
+// Column-major scores of few rows: column splits of at least 64 columns.  Two splits
+// of a long list's row cost more for their two lists than they gain (60,000 x 300 with
+// 64 alternatives 91 us whole, 119 in two; 20,000 x 300 90 whole, 76 in four).
 int column_splits(int64_t n, int32_t d, int32_t k) {
   const int64_t tiles = (n + 63) / 64;
-  const int least = 4 * k > 64 ? 4 * k : 64;
   int64_t s = tiles >= WANT_WAVES ? 1 : WANT_WAVES / tiles;
-  if (s > d / least) s = d / least;
+  if (s > d / 64) s = d / 64;
   if (s > MAX_SPLITS) s = MAX_SPLITS;
-  return s < 1 ? 1 : (int)s;
+  return s < 1 || (s == 2 && k > 32) ? 1 : (int)s;
 }
 
 template <template <int> class Launch, typename... Args>
