@@ -140,7 +140,7 @@ constexpr int TILE_B = 144;    // bytes of a row's 128 in the LDS tile: lanes' 1
 // subnormal; no double of a class rounds to another score.  (+inf, which has no room
 // for a class, counts as the largest finite score.)
 __device__ inline double place_of(float x, int j) {
-  const double v = (double)(fminf(x, FLT_MAX) + 0.0f);
+  const double v = (double)(__builtin_amdgcn_fmed3f(x, -FLT_MAX, FLT_MAX) + 0.0f);
   const uint32_t low = __double2loint(v) | (x < 0.0f ? (uint32_t)j : 0xffffu - (uint32_t)j);
   return __hiloint2double(__double2hiint(v), (int)low);
 }
@@ -155,6 +155,12 @@ __device__ inline double keep_larger(double& v, double p) {
   // in one piece, so that v stays in its registers
   asm("v_min_f64 %1, %0, %2\n\tv_max_f64 %0, %0, %2" : "+v"(v), "=&v"(r) : "v"(p));
   return r;
+}
+
+// bits = 2 bits + (x > y), the comparison's carry in one addition (two wait states
+// between a vector comparison and a vector instruction that reads its mask).
+__device__ inline void push_bit_if_above(uint32_t& bits, float x, float y) {
+  asm("v_cmp_gt_f32 vcc, %1, %2\n\ts_nop 1\n\tv_addc_co_u32 %0, vcc, %0, %0, vcc" : "+v"(bits) : "v"(x), "v"(y) : "vcc");
 }
 
 // Places in a lane's queue (long lists only).
@@ -285,23 +291,21 @@ struct LaneRow {
     if (KM > 0 && !QUEUED && first) {
       start(x, j0, a.k);
     } else if (KM > 0 && (__any(news) || (QUEUED && end))) {
-      // a bit per column above the list's last place, the first column highest;
-      // then the lanes' columns one after the other
+      // a bit per column above the list's last place, then the lanes' columns one after
+      // the other, the first one first
       uint32_t bits = 0;
 #pragma unroll
-      for (int i = 0; i < CH; ++i) bits = 2 * bits + (x[i] > last);
+      for (int i = CH - 1; i >= 0; --i) push_bit_if_above(bits, x[i], last);
       do {
-        const int i = CH - 32 + __builtin_clz(bits | 1);
-        const double p = place_of(again(i), j0 + i);
-        if constexpr (QUEUED) {
-          if (bits) queue[queued * 64] = p;
-          queued += bits != 0;
-          bits &= ~(1u << (CH - 1 - i));
-          if (__any(queued == QUEUE) || (end && !__any(bits != 0))) take(queue);
-        } else {
-          insert(bits ? p : -INFINITY);
-          bits &= ~(1u << (CH - 1 - i));
+        if (bits) {
+          const int i = __builtin_ctz(bits);
+          const double p = place_of(again(i), j0 + i);
+          if constexpr (QUEUED) queue[queued++ * 64] = p;
+          else insert(p);
         }
+        bits &= bits - 1;
+        if constexpr (QUEUED)
+          if (__any(queued == QUEUE) || (end && !__any(bits != 0))) take(queue);
       } while (__any(bits != 0));
       find_last(a.k);
     }
