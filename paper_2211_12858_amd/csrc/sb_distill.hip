@@ -27,6 +27,7 @@
 //
 // exp(z / T) is 2^(z * log2(e) / T) by the hardware's exponential, which returns 0
 // below 2^-126: probabilities under 2^-126 of the row's largest are 0.
+#include <cfloat>
 #include <cmath>
 #include <type_traits>
 
@@ -163,31 +164,29 @@ __device__ inline double tile_norms(const float* tile, int lane) {
   return acc;
 }
 
-template <int ROWS, int C, int MODE, bool MIX, bool FULLC>
-__device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
-  constexpr int PARTS = 64 / ROWS;
-  constexpr int CG = C < 16 ? C : 16, S = CG + 4, NG = C / CG;
-  const DistillArgs& a = r.a;
-  const int W = r.waves, K = a.k;
-  const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = lane / ROWS;
-  Listed* ent = reinterpret_cast<Listed*>(lds);
-  float* red = reinterpret_cast<float*>(lds) + 2 * K * ROWS;  // [DISTILL_RED][W][64]
-  float* tile = red + DISTILL_RED * W * 64 + w * distill_tile_floats(C);
-  float* trow = tile + lane * S;
-  const int j0 = w * C * PARTS;    // the wave's first column
-  int last = a.d - 1 - j0;         // its last one, from there
-  const int jl = j0 + hb * C;      // the lane's first column
-  constexpr bool STEP = FULLC || PARTS == 1;  // a column is a step of a uniform pointer
-  auto at = [&](int i, uint32_t loc, int64_t ld) -> uint32_t {
+// What a wave of k_distill_regs knows of its columns and lanes, and the exchange of
+// values between the waves of a row tile.
+template <int ROWS, int C, bool FULLC>
+struct WaveTile {
+  static constexpr int PARTS = 64 / ROWS;
+  static constexpr bool STEP = FULLC || PARTS == 1;  // a column is a step of a uniform pointer
+  const DistillArgs& a;
+  float* red;  // [DISTILL_RED][W][64]
+  int W, w, lane, rl, hb;
+  int groups, rg;
+  int j0, last;  // the wave's first column, and its last one from there
+
+  // byte offset of column i of the lane's in row `loc` of the tile
+  __device__ uint32_t at(int i, uint32_t loc, int64_t ld) const {
     if (PARTS == 1) return 4 * loc;
     if (FULLC) return 4 * (loc + (uint32_t)(hb * C) * (uint32_t)ld);
     const int c = hb * C + i;
     return 4 * (loc + (uint32_t)(c < last ? c : last) * (uint32_t)ld);
-  };
+  }
   // Rows past the end are row n - 1 again: they store its own values once more
   // and stay out of the norms.
-  auto rows_of = [&](int tile_no, int64_t& base, uint32_t& loc) {
-    base = ((int64_t)tile_no * r.groups + rg) * ROWS;
+  __device__ void rows_of(int tile_no, int64_t& base, uint32_t& loc) const {
+    base = ((int64_t)tile_no * groups + rg) * ROWS;
     const int64_t left = a.n - 1 - base;
     if (left < 0) {
       base = a.n - 1;
@@ -195,48 +194,188 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     } else {
       loc = rl < left ? rl : (uint32_t)left;
     }
-  };
+  }
+  __device__ void load(float (&x)[C], int64_t base, uint32_t loc) const {
+    const float* p = a.F + (int64_t)j0 * a.ld_f + base;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      x[i] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + at(i, loc, a.ld_f));
+      if (STEP && (FULLC || i < last)) p += a.ld_f;
+    }
+  }
+  __device__ void put(int q, float v) const { red[(q * W + w) * 64 + lane] = v; }
+  __device__ float max_of(int q) const {
+    float v = red[q * W * 64 + lane];
+    for (int u = 1; u < W; ++u) v = fmaxf(v, red[(q * W + u) * 64 + lane]);
+    return v;
+  }
+  __device__ float sum_of(int q) const {
+    float v = red[q * W * 64 + lane];
+    for (int u = 1; u < W; ++u) v += red[(q * W + u) * 64 + lane];
+    return v;
+  }
+  // over the lanes of a row
+  __device__ float part_sum(float v) const {
+#pragma unroll
+    for (int off = 32; off >= ROWS; off >>= 1) v += __shfl_xor(v, off, 64);
+    return v;
+  }
+  __device__ float part_max(float v) const {
+#pragma unroll
+    for (int off = 32; off >= ROWS; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
+    return v;
+  }
+};
+
+// The loss alone: each wave reads the scores of the classes that its share of the
+// places lists, which its block's columns have just brought, so nothing goes through
+// the tile and the next tile's scores are on their way from the sums on.
+template <int ROWS, int C, bool MIX, bool FULLC>
+__device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
+  constexpr int PARTS = 64 / ROWS;
+  const DistillArgs& a = r.a;
+  const int W = r.waves, K = a.k;
+  const int lane = threadIdx.x & 63, hb = lane / ROWS;
+  const WaveTile<ROWS, C, FULLC> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, lane & (ROWS - 1), hb,
+                                    r.groups, rg, w * C * PARTS, a.d - 1 - w * C * PARTS};
+  const int s0 = w * PARTS + hb, step = W * PARTS;
+  int64_t base;
+  uint32_t loc;
+  wt.rows_of(bx, base, loc);
+  float x[C];
+  wt.load(x, base, loc);
+  constexpr int AHEAD = 4;
+  Place ahead[AHEAD];
+#pragma unroll
+  for (int u = 0; u < AHEAD; ++u) {
+    ahead[u] = Place{-1, 0.0f};
+    if (s0 + u * step < K) ahead[u] = load_place(a, s0 + u * step, base + loc);
+  }
+  int next_y = a.w > 0.0 ? a.labels[base + loc] : -1;
+  for (int t = bx; t < r.tiles; t += grid) {
+    const int64_t row = base + loc;
+    auto score = [&](int id) { return id >= 0 ? a.F[(int64_t)id * a.ld_f + row] : 0.0f; };
+    Place now[AHEAD];
+    float xc[AHEAD];
+    float vm = -INFINITY;
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u) {
+      now[u] = usable(a, ahead[u]);
+      xc[u] = score(now[u].id);
+      vm = fmaxf(vm, now[u].v);
+    }
+#pragma unroll 4
+    for (int sl = s0 + AHEAD * step; sl < K; sl += step) vm = fmaxf(vm, usable(a, load_place(a, sl, row)).v);
+    const int y = next_y < a.d ? next_y : -1;
+    const float xy = w == 0 ? score(y) : 0.0f;
+    float m = x[0];
+#pragma unroll
+    for (int i = 1; i < C; ++i) m = fmaxf(m, x[i]);
+    m = wt.part_max(m);
+    vm = wt.part_max(vm);
+    if (W > 1) {
+      wt.put(0, m);
+      wt.put(1, vm);
+      lds_barrier();
+      m = wt.max_of(0);
+      vm = wt.max_of(1);
+    }
+    float s1 = 0.0f, sT = 0.0f;
+#pragma unroll
+    for (int i = 0; i < C; ++i) {
+      const float z = x[i] - m;
+      const bool live = FULLC || hb * C + i <= wt.last;
+      const float e = exp2_hw(z * r.c2);
+      sT += live ? e : 0.0f;
+      if (MIX) {
+        const float e1 = exp2_hw(z * LOG2E);
+        s1 += live ? e1 : 0.0f;
+      }
+    }
+    asm volatile("" : "+v"(sT), "+v"(s1));
+    // the next tile, past the last one this one again
+    int64_t nbase;
+    uint32_t nloc;
+    wt.rows_of(t + grid < r.tiles ? t + grid : t, nbase, nloc);
+    wt.load(x, nbase, nloc);
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u * step < K) ahead[u] = load_place(a, s0 + u * step, nbase + nloc);
+    if (a.w > 0.0) next_y = a.labels[nbase + nloc];
+    float zs = 0.0f, us = 0.0f, ds = 0.0f;  // ds: sum e_t (a_c - m)
+    auto add = [&](const Place& p, float score_c) {
+      const float e = place_exp(r, p.v, vm, us);
+      zs += e;
+      if (p.id >= 0) ds = fmaf(e, score_c - m, ds);
+    };
+#pragma unroll
+    for (int u = 0; u < AHEAD; ++u)
+      if (s0 + u * step < K) add(now[u], xc[u]);
+#pragma unroll 4
+    for (int sl = s0 + AHEAD * step; sl < K; sl += step) {
+      const Place p = usable(a, load_place(a, sl, row));
+      add(p, score(p.id));
+    }
+    zs = wt.part_sum(zs);
+    us = wt.part_sum(us);
+    ds = wt.part_sum(ds);
+    sT = wt.part_sum(sT);
+    if (MIX) s1 = wt.part_sum(s1);
+    if (W > 1) {
+      wt.put(2, zs);
+      wt.put(3, us);
+      wt.put(4, sT);
+      if (MIX) wt.put(5, s1);
+      wt.put(6, ds);
+      lds_barrier();
+    }
+    if (w == 0) {
+      if (W > 1) {
+        zs = wt.sum_of(2);
+        us = wt.sum_of(3);
+        sT = wt.sum_of(4);
+        if (MIX) s1 = wt.sum_of(5);
+        ds = wt.sum_of(6);
+      }
+      if (!MIX) s1 = sT;
+      const Teacher te = teacher_of(r, zs, us);
+      const float A = y >= 0 ? r.w : 0.0f;
+      const float dot = fmaf(te.wt, ds, y >= 0 ? A * (xy - m) : 0.0f);
+      if (hb == 0) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
+    }
+    base = nbase;
+    loc = nloc;
+  }
+}
+
+// MODE 1: the gradients; 2: the hessians or their row sums too.
+template <int ROWS, int C, int MODE, bool MIX, bool FULLC>
+__device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
+  constexpr int PARTS = 64 / ROWS;
+  constexpr int CG = C < 16 ? C : 16, S = CG + 4, NG = C / CG;
+  constexpr bool STEP = WaveTile<ROWS, C, FULLC>::STEP;
+  const DistillArgs& a = r.a;
+  const int W = r.waves, K = a.k;
+  const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = lane / ROWS;
+  Listed* ent = reinterpret_cast<Listed*>(lds);
+  const int j0 = w * C * PARTS;  // the wave's first column
+  const int jl = j0 + hb * C;    // the lane's first column
+  WaveTile<ROWS, C, FULLC> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, rl, hb, r.groups, rg, j0,
+                              a.d - 1 - j0};
+  int& last = wt.last;
+  float* tile = wt.red + DISTILL_RED * W * 64 + w * distill_tile_floats(C);
+  float* trow = tile + lane * S;
   auto load_at = [](const float* p, uint32_t bytes) {
     return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + bytes);
   };
   auto store_at = [](float* p, uint32_t bytes, float v) {
     *reinterpret_cast<float*>(reinterpret_cast<char*>(p) + bytes) = v;
   };
-  auto red_put = [&](int q, float v) { red[(q * W + w) * 64 + lane] = v; };
-  auto red_max = [&](int q) {
-    float v = red[q * W * 64 + lane];
-    for (int u = 1; u < W; ++u) v = fmaxf(v, red[(q * W + u) * 64 + lane]);
-    return v;
-  };
-  auto red_sum = [&](int q) {
-    float v = red[q * W * 64 + lane];
-    for (int u = 1; u < W; ++u) v += red[(q * W + u) * 64 + lane];
-    return v;
-  };
-  // over the lanes of a row
-  auto part_sum = [&](float v) {
-#pragma unroll
-    for (int off = 32; off >= ROWS; off >>= 1) v += __shfl_xor(v, off, 64);
-    return v;
-  };
-  auto part_max = [&](float v) {
-#pragma unroll
-    for (int off = 32; off >= ROWS; off >>= 1) v = fmaxf(v, __shfl_xor(v, off, 64));
-    return v;
-  };
-
   int64_t base;
   uint32_t loc;
-  rows_of(bx, base, loc);
+  wt.rows_of(bx, base, loc);
   float x[C];
-  {
-    const float* p = a.F + (int64_t)j0 * a.ld_f + base;
-#pragma unroll
-    for (int i = 0; i < C; ++i) {
-      x[i] = load_at(p, at(i, loc, a.ld_f));
-      if (STEP && (FULLC || i < last)) p += a.ld_f;
-    }
-  }
+  wt.load(x, base, loc);
   // the first places of the wave, and the labels, a tile ahead
   constexpr int AHEAD = PARTS == 1 ? 4 : 2;
   const int s0 = w * PARTS + hb;
@@ -267,14 +406,14 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     float m = x[0];
 #pragma unroll
     for (int i = 1; i < C; ++i) m = fmaxf(m, x[i]);
-    m = part_max(m);
-    vm = part_max(vm);
+    m = wt.part_max(m);
+    vm = wt.part_max(vm);
     if (W > 1) {
-      red_put(0, m);
-      red_put(1, vm);
+      wt.put(0, m);
+      wt.put(1, vm);
       lds_barrier();
-      m = red_max(0);
-      vm = red_max(1);
+      m = wt.max_of(0);
+      vm = wt.max_of(1);
     } else {
       wave_sync();
     }
@@ -298,20 +437,20 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
         s1 += live ? e1 : 0.0f;
       }
     }
-    zs = part_sum(zs);
-    us = part_sum(us);
-    sT = part_sum(sT);
-    if (MIX) s1 = part_sum(s1);
+    zs = wt.part_sum(zs);
+    us = wt.part_sum(us);
+    sT = wt.part_sum(sT);
+    if (MIX) s1 = wt.part_sum(s1);
     if (W > 1) {
-      red_put(2, zs);
-      red_put(3, us);
-      red_put(4, sT);
-      if (MIX) red_put(5, s1);
+      wt.put(2, zs);
+      wt.put(3, us);
+      wt.put(4, sT);
+      if (MIX) wt.put(5, s1);
       lds_barrier();
-      zs = red_sum(2);
-      us = red_sum(3);
-      sT = red_sum(4);
-      if (MIX) s1 = red_sum(5);
+      zs = wt.sum_of(2);
+      us = wt.sum_of(3);
+      sT = wt.sum_of(4);
+      if (MIX) s1 = wt.sum_of(5);
     } else {
       wave_sync();
     }
@@ -326,7 +465,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     asm volatile("" : "+v"(m));
     int64_t nbase;
     uint32_t nloc;
-    rows_of(t + grid < r.tiles ? t + grid : t, nbase, nloc);
+    wt.rows_of(t + grid < r.tiles ? t + grid : t, nbase, nloc);
     // the next tile's places and labels, which arrive while this one goes out
     const int64_t nrow = nbase + nloc;
 #pragma unroll
@@ -334,28 +473,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       if (s0 + u * W * PARTS < K) ahead[u] = load_place(a, s0 + u * W * PARTS, nrow);
     if (a.w > 0.0) next_y = a.labels[nrow];
     float hsum = 0.0f, dot = 0.0f;
-    if (MODE == 0) {
-      // the loss alone: the scores of the listed classes, through the tile
-#pragma unroll
-      for (int g = 0; g < NG; ++g) {
-        wave_sync();
-#pragma unroll
-        for (int i = 0; i < CG; ++i) trow[i] = x[g * CG + i];
-        for (int sl = 0; sl < K; ++sl) {
-          const Listed p = ent[sl * ROWS + rl];
-          const uint32_t c = (uint32_t)(p.id - jl - g * CG);
-          if (c < CG) dot += te.wt * p.e * (trow[c] - m);
-        }
-        const uint32_t cy = (uint32_t)(y - jl - g * CG);
-        if (y >= 0 && cy < CG) dot += A * (trow[cy] - m);
-      }
-      const float* p = a.F + (int64_t)j0 * a.ld_f + nbase;
-#pragma unroll
-      for (int i = 0; i < C; ++i) {
-        x[i] = load_at(p, at(i, nloc, a.ld_f));
-        if (STEP && (FULLC || i < last)) p += a.ld_f;
-      }
-    } else {
+    {
       // the leading dimensions are seen anew at every step: all column offsets
       // would otherwise be formed before the loop and held, spilled, across it
       int64_t ld_f = a.ld_f, ld_g = a.ld_g, ld_h = a.ld_h;
@@ -389,7 +507,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
             }
             dot = fmaf(tv[u], z, dot);
             // columns past the last repeat it: same address, same value, but no target there
-            if (live) store_at(Gc, at(i, loc, ld_g), gr);
+            if (live) store_at(Gc, wt.at(i, loc, ld_g), gr);
             if (MODE == 2) {
               const float pT = eT * iT;
               float h = hT * fmaf(-pT, pT, pT);
@@ -400,12 +518,12 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
               hsum += live ? h : 0.0f;
               if (a.hess) {
                 asm volatile("" : "+s"(ld_h));
-                if (live) store_at(Hc, at(i, loc, ld_h), h);
+                if (live) store_at(Hc, wt.at(i, loc, ld_h), h);
                 if (STEP && (FULLC || i < last)) Hc += ld_h;
               }
             }
             gv[u] = ok && live ? gr : 0.0f;
-            x[i] = load_at(Fc, at(i, nloc, ld_f));
+            x[i] = load_at(Fc, wt.at(i, nloc, ld_f));
             if (STEP && (FULLC || i < last)) {
               Fc += ld_f;
               Gc += ld_g;
@@ -425,20 +543,20 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       }
     }
     if (W > 1 || a.loss || a.h_row) {
-      if (a.loss) dot = part_sum(dot);
-      if (MODE == 2 && a.h_row) hsum = part_sum(hsum);
+      if (a.loss) dot = wt.part_sum(dot);
+      if (MODE == 2 && a.h_row) hsum = wt.part_sum(hsum);
       if (W > 1) {
-        if (a.loss) red_put(6, dot);
-        if (MODE == 2 && a.h_row) red_put(7, hsum);
+        if (a.loss) wt.put(6, dot);
+        if (MODE == 2 && a.h_row) wt.put(7, hsum);
         lds_barrier();  // and all waves are through with the places
       }
       if (w == 0 && hb == 0) {
         if (a.loss) {
-          if (W > 1) dot = red_sum(6);
+          if (W > 1) dot = wt.sum_of(6);
           a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
         }
         if (MODE == 2 && a.h_row) {
-          if (W > 1) hsum = red_sum(7);
+          if (W > 1) hsum = wt.sum_of(7);
           a.h_row[row] = hsum * (1.0f / (float)a.d);
         }
       }
@@ -447,7 +565,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     base = nbase;
     loc = nloc;
   }
-  if (MODE != 0 && r.npart) {
+  if (r.npart) {
     // the row segments of a column, in order
     const int c = lane % CG;
 #pragma unroll
@@ -473,8 +591,110 @@ __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs
   const int rg = wv / r.waves, w = wv - rg * r.waves;
   const int bytes = 4 * (2 * r.a.k * ROWS + DISTILL_RED * r.waves * 64 + r.waves * distill_tile_floats(C));
   char* lds = smem + rg * bytes;
-  if ((w + 1) * C * (64 / ROWS) <= r.a.d) distill_wave<ROWS, C, MODE, MIX, true>(r, lds, w, rg, bx, grid);
-  else distill_wave<ROWS, C, MODE, MIX, false>(r, lds, w, rg, bx, grid);
+  const bool full = (w + 1) * C * (64 / ROWS) <= r.a.d;  // all columns of the wave exist
+  if constexpr (MODE == 0) {
+    if (full) loss_wave<ROWS, C, MIX, true>(r, lds, w, rg, bx, grid);
+    else loss_wave<ROWS, C, MIX, false>(r, lds, w, rg, bx, grid);
+  } else {
+    if (full) distill_wave<ROWS, C, MODE, MIX, true>(r, lds, w, rg, bx, grid);
+    else distill_wave<ROWS, C, MODE, MIX, false>(r, lds, w, rg, bx, grid);
+  }
+}
+
+// ---------------------------------------------------------------- the loss of many rows
+// One lane per row, one wave per 64-row tile: a running maximum and sums over the
+// columns in order, then the places, eight at a time, with a running maximum of
+// their own.  No wave waits for another.
+template <bool MIX>
+__global__ void __launch_bounds__(256) k_loss_by_lane(RowArgs r) {
+  const DistillArgs& a = r.a;
+  const int lane = threadIdx.x & 63;
+  const int64_t base = ((int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * 64;
+  if (base >= a.n) return;
+  const int64_t left = a.n - 1 - base;  // rows past the end read row n - 1 and store nothing
+  const int loc = lane < left ? lane : (int)left;
+  const int64_t row = base + loc;
+  const float* F = a.F + base;
+  float m = -FLT_MAX, s1 = 0.0f, sT = 0.0f;
+  float x[2][16];
+  auto load = [&](float (&to)[16], int j) {
+    const float* p = F + (int64_t)j * a.ld_f;
+    if (j + 16 <= a.d) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, p += a.ld_f) to[i] = p[loc];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, p += a.ld_f) {
+        to[i] = -INFINITY;
+        if (j + i < a.d) to[i] = p[loc];
+      }
+    }
+  };
+  auto step = [&](const float (&now)[16]) {
+    float mn = m;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mn = fmaxf(mn, now[i]);
+    float a1 = 0.0f, aT = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float z = now[i] - mn;
+      aT += exp2_hw(z * r.c2);
+      if (MIX) a1 += exp2_hw(z * LOG2E);
+      if (i % 4 == 3) asm volatile("" : "+v"(aT), "+v"(a1));  // here and now: put off, the terms take registers
+    }
+    sT = fmaf(sT, exp2_hw((m - mn) * r.c2), aT);
+    if (MIX) s1 = fmaf(s1, exp2_hw((m - mn) * LOG2E), a1);
+    m = mn;
+  };
+  load(x[0], 0);
+  for (int j = 0; j < a.d; j += 32) {
+    if (j + 16 < a.d) load(x[1], j + 16);
+    step(x[0]);
+    if (j + 16 < a.d) {
+      if (j + 32 < a.d) load(x[0], j + 32);
+      step(x[1]);
+    }
+  }
+  if (!MIX) s1 = sT;
+  const bool logits = a.teacher == SB_TEACHER_LOGITS;
+  float vm = logits ? -FLT_MAX : 0.0f, zs = 0.0f, us = 0.0f, ds = 0.0f;
+  for (int s = 0; s < a.k; s += 8) {
+    Place p[8];
+    float xc[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) p[u] = s + u < a.k ? load_place(a, s + u, row) : Place{-1, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      p[u] = usable(a, p[u]);
+      xc[u] = p[u].id >= 0 ? F[(int64_t)p[u].id * a.ld_f + loc] : m;
+    }
+    if (logits) {
+      float vn = vm;
+#pragma unroll
+      for (int u = 0; u < 8; ++u) vn = fmaxf(vn, p[u].v);
+      const float du = fmaxf((vm - vn) * r.inv_t, -1000.0f), f = exp2_hw(du * LOG2E);
+      us = f * fmaf(zs, du, us);
+      zs *= f;
+      ds *= f;
+      vm = vn;
+    }
+#pragma unroll
+    for (int u = 0; u < 8; ++u) {
+      const float e = place_exp(r, p[u].v, vm, us);
+      zs += e;
+      ds = fmaf(e, xc[u] - m, ds);
+    }
+  }
+  const Teacher te = teacher_of(r, zs, us);
+  float dot = te.wt * ds, A = 0.0f;
+  if (a.w > 0.0) {
+    const int y = a.labels[row];
+    if (y >= 0 && y < a.d) {
+      A = r.w;
+      dot = fmaf(A, F[(int64_t)y * a.ld_f + loc] - m, dot);
+    }
+  }
+  if (lane <= left) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
 }
 
 // ---------------------------------------------------------------- wider rows
@@ -790,6 +1010,12 @@ __global__ void __launch_bounds__(256) k_distill_hrow(const float* sums, int ran
   h_row[i] = s * (1.0f / (float)d);
 }
 
+// The loss alone, a wave per tile: where there are tiles for the waves of the card, and
+// few listed scores, which by then are read from memory once more, a cache line each
+// (100,000 x 1000: 10 places 87 us, 143 by blocks; 300,007 rows: x 400, 10 places 135 and
+// 142, x 1000, 32 places 379 and 380; 1M x 100, 10 places 157 and 131).
+bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 40 * a.k; }
+
 bool in_regs(const DistillArgs& a) {
   if (a.d > DISTILL_REGS_MAX_D) return false;
   if (a.d <= DISTILL_ONE_PART_D) return true;
@@ -859,7 +1085,11 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
   r.npart = a.norm2 ? static_cast<double*>(ws) : nullptr;
   const bool mix = a.w > 0.0 && a.T != 1.0;
   const int mode = !a.G ? 0 : a.hess || a.h_row ? 2 : 1;
-  if (in_regs(a)) {
+  if (mode == 0 && loss_by_lane(a)) {
+    const dim3 blocks((unsigned)((a.n + 255) / 256));
+    if (mix) hipLaunchKernelGGL(k_loss_by_lane<true>, blocks, dim3(256), 0, st, r);
+    else hipLaunchKernelGGL(k_loss_by_lane<false>, blocks, dim3(256), 0, st, r);
+  } else if (in_regs(a)) {
     const DistillPlan p = distill_plan(a.n, a.d, a.k);
     r.waves = p.waves;
     r.groups = p.groups;

@@ -176,7 +176,9 @@ def test_shapes(n, d, k, kind, T, w):
 @pytest.mark.parametrize("n,d,k,kind,T,w", [(200_003, 10, 3, "logits", 1.0, 0.5), (150_001, 30, 30, "log_probs", 2.0, 0.2),
                                             (100_007, 100, 10, "logits", 2.0, 0.3), (30_011, 300, 64, "logits", 1.5, 0.0),
                                             (20_001, 600, 8, "log_probs", 1.0, 0.0), (12_345, 1000, 32, "logits", 4.0, 0.1),
-                                            (9_001, 1500, 16, "logits", 2.0, 0.5)])
+                                            (9_001, 1500, 16, "logits", 2.0, 0.5), (100_003, 370, 9, "logits", 2.0, 0.4),
+                                            (100_001, 41, 1, "log_probs", 1.0, 0.0),
+                                            (100_031, 1030, 10, "logits", 0.8, 0.0)])
 def test_many_rows(n, d, k, kind, T, w):
     print("case: distill", n, d, k, kind, T, w, flush=True)
     rng = np.random.default_rng(n + d + k)
