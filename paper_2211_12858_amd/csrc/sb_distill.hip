@@ -166,7 +166,8 @@ __device__ inline double tile_norms(const float* tile, int lane) {
 
 // What a wave of k_distill_regs knows of its columns and lanes, and the exchange of
 // values between the waves of a row tile.
-template <int ROWS, int C, bool FULLC>
+// OFF: unsigned 64 bits where a row's lanes are columns further apart than 32 cover.
+template <int ROWS, int C, bool FULLC, typename OFF>
 struct WaveTile {
   static constexpr int PARTS = 64 / ROWS;
   static constexpr bool STEP = FULLC || PARTS == 1;  // a column is a step of a uniform pointer
@@ -177,11 +178,11 @@ struct WaveTile {
   int j0, last;  // the wave's first column, and its last one from there
 
   // byte offset of column i of the lane's in row `loc` of the tile
-  __device__ uint32_t at(int i, uint32_t loc, int64_t ld) const {
+  __device__ OFF at(int i, uint32_t loc, int64_t ld) const {
     if (PARTS == 1) return 4 * loc;
-    if (FULLC) return 4 * (loc + (uint32_t)(hb * C) * (uint32_t)ld);
+    if (FULLC) return 4 * (loc + (OFF)(hb * C) * (OFF)ld);
     const int c = hb * C + i;
-    return 4 * (loc + (uint32_t)(c < last ? c : last) * (uint32_t)ld);
+    return 4 * (loc + (OFF)(c < last ? c : last) * (OFF)ld);
   }
   // Rows past the end are row n - 1 again: they store its own values once more
   // and stay out of the norms.
@@ -230,13 +231,13 @@ struct WaveTile {
 // The loss alone: each wave reads the scores of the classes that its share of the
 // places lists, which its block's columns have just brought, so nothing goes through
 // the tile and the next tile's scores are on their way from the sums on.
-template <int ROWS, int C, bool MIX, bool FULLC>
+template <int ROWS, int C, bool MIX, bool FULLC, typename OFF>
 __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
   constexpr int PARTS = 64 / ROWS;
   const DistillArgs& a = r.a;
   const int W = r.waves, K = a.k;
   const int lane = threadIdx.x & 63, hb = lane / ROWS;
-  const WaveTile<ROWS, C, FULLC> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, lane & (ROWS - 1), hb,
+  const WaveTile<ROWS, C, FULLC, OFF> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, lane & (ROWS - 1), hb,
                                     r.groups, rg, w * C * PARTS, a.d - 1 - w * C * PARTS};
   const int s0 = w * PARTS + hb, step = W * PARTS;
   int64_t base;
@@ -349,26 +350,26 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
 }
 
 // MODE 1: the gradients; 2: the hessians or their row sums too.
-template <int ROWS, int C, int MODE, bool MIX, bool FULLC>
+template <int ROWS, int C, int MODE, bool MIX, bool FULLC, typename OFF>
 __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
   constexpr int PARTS = 64 / ROWS;
   constexpr int CG = C < 16 ? C : 16, S = CG + 4, NG = C / CG;
-  constexpr bool STEP = WaveTile<ROWS, C, FULLC>::STEP;
+  constexpr bool STEP = WaveTile<ROWS, C, FULLC, OFF>::STEP;
   const DistillArgs& a = r.a;
   const int W = r.waves, K = a.k;
   const int lane = threadIdx.x & 63, rl = lane & (ROWS - 1), hb = lane / ROWS;
   Listed* ent = reinterpret_cast<Listed*>(lds);
   const int j0 = w * C * PARTS;  // the wave's first column
   const int jl = j0 + hb * C;    // the lane's first column
-  WaveTile<ROWS, C, FULLC> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, rl, hb, r.groups, rg, j0,
+  WaveTile<ROWS, C, FULLC, OFF> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, rl, hb, r.groups, rg, j0,
                               a.d - 1 - j0};
   int& last = wt.last;
   float* tile = wt.red + DISTILL_RED * W * 64 + w * distill_tile_floats(C);
   float* trow = tile + lane * S;
-  auto load_at = [](const float* p, uint32_t bytes) {
+  auto load_at = [](const float* p, OFF bytes) {
     return *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + bytes);
   };
-  auto store_at = [](float* p, uint32_t bytes, float v) {
+  auto store_at = [](float* p, OFF bytes, float v) {
     *reinterpret_cast<float*>(reinterpret_cast<char*>(p) + bytes) = v;
   };
   int64_t base;
@@ -582,7 +583,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
 // Blocks go to the 8 XCDs in turn; each XCD takes a run of neighbouring tiles, which
 // share cache lines where columns do not start on a line.  The launch has a multiple
 // of 8 blocks.
-template <int ROWS, int C, int MODE, bool MIX>
+template <int ROWS, int C, int MODE, bool MIX, typename OFF>
 __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs r, int grid) {
   extern __shared__ __align__(16) char smem[];
   const int bx = (int)(blockIdx.x & 7) * ((grid + 7) >> 3) + (int)(blockIdx.x >> 3);
@@ -593,11 +594,11 @@ __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs
   char* lds = smem + rg * bytes;
   const bool full = (w + 1) * C * (64 / ROWS) <= r.a.d;  // all columns of the wave exist
   if constexpr (MODE == 0) {
-    if (full) loss_wave<ROWS, C, MIX, true>(r, lds, w, rg, bx, grid);
-    else loss_wave<ROWS, C, MIX, false>(r, lds, w, rg, bx, grid);
+    if (full) loss_wave<ROWS, C, MIX, true, OFF>(r, lds, w, rg, bx, grid);
+    else loss_wave<ROWS, C, MIX, false, OFF>(r, lds, w, rg, bx, grid);
   } else {
-    if (full) distill_wave<ROWS, C, MODE, MIX, true>(r, lds, w, rg, bx, grid);
-    else distill_wave<ROWS, C, MODE, MIX, false>(r, lds, w, rg, bx, grid);
+    if (full) distill_wave<ROWS, C, MODE, MIX, true, OFF>(r, lds, w, rg, bx, grid);
+    else distill_wave<ROWS, C, MODE, MIX, false, OFF>(r, lds, w, rg, bx, grid);
   }
 }
 
@@ -1014,28 +1015,24 @@ __global__ void __launch_bounds__(256) k_distill_hrow(const float* sums, int ran
 // few listed scores, which by then are read from memory once more, a cache line each
 // (100,000 x 1000: 10 places 87 us, 143 by blocks; 300,007 rows: x 400, 10 places 135 and
 // 142, x 1000, 32 places 379 and 380; 1M x 100, 10 places 157 and 131).
-bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 40 * a.k; }
+bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 30 * a.k; }
 
-bool in_regs(const DistillArgs& a) {
-  if (a.d > DISTILL_REGS_MAX_D) return false;
-  if (a.d <= DISTILL_ONE_PART_D) return true;
-  return a.ld_f < DISTILL_PARTS_MAX_LD && (!a.G || a.ld_g < DISTILL_PARTS_MAX_LD) &&
-         (!a.hess || a.ld_h < DISTILL_PARTS_MAX_LD);
-}
-
-template <int ROWS, int C, int MODE>
+template <int ROWS, int C, int MODE, typename OFF>
 void launch_regs(const RowArgs& r, const DistillPlan& p, bool mix, hipStream_t st) {
   const dim3 grid((p.grid + 7) / 8 * 8), block(64 * p.waves * p.groups);
-  if (mix) hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, true>), grid, block, p.lds, st, r, p.grid);
-  else hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, false>), grid, block, p.lds, st, r, p.grid);
+  if (mix) hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, true, OFF>), grid, block, p.lds, st, r, p.grid);
+  else hipLaunchKernelGGL((k_distill_regs<ROWS, C, MODE, false, OFF>), grid, block, p.lds, st, r, p.grid);
 }
 
 template <int MODE>
 void launch_mode(const RowArgs& r, const DistillPlan& p, bool mix, hipStream_t st) {
-  if (p.rows == 32) launch_regs<32, 32, MODE>(r, p, mix, st);
-  else if (p.c == 32) launch_regs<64, 32, MODE>(r, p, mix, st);
-  else if (p.c == 16) launch_regs<64, 16, MODE>(r, p, mix, st);
-  else launch_regs<64, 8, MODE>(r, p, mix, st);
+  const DistillArgs& a = r.a;
+  const bool near = a.ld_f < DISTILL_NEAR_LD && (!a.G || a.ld_g < DISTILL_NEAR_LD) && (!a.hess || a.ld_h < DISTILL_NEAR_LD);
+  if (p.rows == 32 && near) launch_regs<32, 32, MODE, uint32_t>(r, p, mix, st);
+  else if (p.rows == 32) launch_regs<32, 32, MODE, uint64_t>(r, p, mix, st);
+  else if (p.c == 32) launch_regs<64, 32, MODE, uint32_t>(r, p, mix, st);
+  else if (p.c == 16) launch_regs<64, 16, MODE, uint32_t>(r, p, mix, st);
+  else launch_regs<64, 8, MODE, uint32_t>(r, p, mix, st);
 }
 
 template <int MODE, bool MIX>
@@ -1054,21 +1051,17 @@ void launch_wide(const RowArgs& r, const DistillWidePlan& p, hipStream_t st) {
 }
 
 int64_t norm_bytes(int64_t n, int32_t d, int32_t k) {
-  int64_t parts = distill_wide_plan(n, d).slots;
-  if (d <= DISTILL_REGS_MAX_D) {
-    const DistillPlan p = distill_plan(n, d, k);
-    if ((int64_t)p.grid * p.groups > parts) parts = (int64_t)p.grid * p.groups;
-  }
-  return align256((int64_t)d * parts * 8);
+  if (d > DISTILL_REGS_MAX_D) return align256((int64_t)d * distill_wide_plan(n, d).slots * 8);
+  const DistillPlan p = distill_plan(n, d, k);
+  return align256((int64_t)d * p.grid * p.groups * 8);
 }
 
 }  // namespace
 
-// Workspace: [norm partials][rows' values and targets][statistics of the ranges]
+// Workspace: [norm partials]; past 1024 classes [rows' values and targets][statistics of the ranges] too
 int64_t distill_ws_bytes(int64_t n, int32_t d, int32_t k) {
   int64_t b = norm_bytes(n, d, k);
-  // narrower rows never take the ranges
-  if (d > DISTILL_ONE_PART_D)
+  if (d > DISTILL_REGS_MAX_D)
     b += align256((int64_t)(ROW_VALUES + k) * n * 4) + align256((int64_t)distill_wide_plan(n, d).ranges * 3 * n * 4);
   return b;
 }
@@ -1089,7 +1082,7 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
     const dim3 blocks((unsigned)((a.n + 255) / 256));
     if (mix) hipLaunchKernelGGL(k_loss_by_lane<true>, blocks, dim3(256), 0, st, r);
     else hipLaunchKernelGGL(k_loss_by_lane<false>, blocks, dim3(256), 0, st, r);
-  } else if (in_regs(a)) {
+  } else if (a.d <= DISTILL_REGS_MAX_D) {
     const DistillPlan p = distill_plan(a.n, a.d, a.k);
     r.waves = p.waves;
     r.groups = p.groups;

@@ -9,8 +9,8 @@ namespace sb {
 constexpr int DISTILL_MAX_WAVES = 16;
 constexpr int DISTILL_REGS_MAX_D = 1024;
 constexpr int DISTILL_ONE_PART_D = 512;
-// where a row has two lanes of a wave, their offsets are 32-bit byte offsets of up to 63 columns
-constexpr int64_t DISTILL_PARTS_MAX_LD = int64_t(1) << 24;
+// where a row has two lanes of a wave, 32-bit byte offsets cover their 63 columns up to here
+constexpr int64_t DISTILL_NEAR_LD = int64_t(1) << 24;
 constexpr int DISTILL_RED = 8;  // per-wave values that a block's waves exchange
 
 // Rows in the registers of a block's waves.
@@ -49,8 +49,7 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
   return p;
 }
 
-// Wider rows (and leading dimensions that the lanes' offsets do not cover): the
-// statistics of column ranges first, then the outputs range by range.
+// Wider rows: the statistics of column ranges first, then the outputs range by range.
 constexpr int DISTILL_RANGE = 512;     // columns per block at most, a quarter per wave
 constexpr int DISTILL_SLOTS = 512;     // row tiles in flight, and norm partials per column at most
 constexpr int DISTILL_BLOCKS = 1024;   // fewer (tile, range) pairs than that take narrower ranges

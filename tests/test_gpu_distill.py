@@ -280,9 +280,10 @@ def test_offsets_past_32_bits():
     check(F, ids, vals, 2.0, 0.5, y, "logits", *run(F, ids, vals, 2.0, 0.5, y, "logits", ld=(1 << 27) + 1))
 
 
-def test_a_leading_dimension_of_2_to_the_24():
+@pytest.mark.parametrize("n,d", [(300, 130), (65, 513), (40, 576)])
+def test_a_leading_dimension_of_2_to_the_24(n, d):
     rng = np.random.default_rng(7)
-    n, d, k = 300, 130, 6
+    k = 6
     F, ids, vals, y = inputs(rng, n, d, k, "logits")
     check(F, ids, vals, 2.0, 0.5, y, "logits", *run(F, ids, vals, 2.0, 0.5, y, "logits", ld=(1 << 24) // 4 + 100))
 
