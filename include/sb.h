@@ -504,7 +504,8 @@ int32_t sb_update_and_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
  *
  * F, dtype, order, ld_f  n x d scores; SB_COLUMN_MAJOR takes SB_F32 only,
  *            SB_ROW_MAJOR every type.  -inf excludes a class (p = 0).  A row
- *            with NaN or +inf gets NaN for logp, lse and entropy.
+ *            with NaN or +inf gets NaN for logp, lse and entropy; its rank and
+ *            alternatives are in range, but no particular ones.
  * temperature  in [1e-4, 1e4].
  * labels     int32, n entries: the given class of every row (may be NULL
  *            if logp and rank are).
@@ -545,7 +546,9 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
  * whose label is outside [0, d) have no first term, rows with no used place
  * no second.
  *
- * F, ld_f      n x d fp32 scores, column-major, finite.
+ * F, ld_f      n x d fp32 scores, column-major.  -inf excludes a class (p = 0):
+ *              it adds nothing but where it is a target, which makes the loss
+ *              +inf.  A row with NaN or +inf gets undefined outputs.
  * temperature  T, in [1e-4, 1e4].  hard_weight in [0, 1].
  * labels       n int32; may be NULL if hard_weight is 0.
  * teacher      SB_TEACHER_*.

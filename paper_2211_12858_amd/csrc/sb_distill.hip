@@ -9,6 +9,7 @@
 //   loss = A log s1 + B T (sum q_t log q_t + Q log sT) - sum_j target_j z_j
 //   g_j  = A p1_j + B Q pT_j - target_j
 //   h_j  = A p1_j (1 - p1_j) + (B / T) Q pT_j (1 - pT_j)
+// (0 log 0 = 0; a score of -inf has p = 0, and a target on it makes the loss +inf),
 // so the teacher's list and the label are one sparse target row, and at T = 1 the
 // two softmaxes are one.
 //
@@ -33,6 +34,8 @@
 
 #include "sb_common.h"
 #include "sb_distill_plan.h"
+
+extern "C" __device__ float sb_mul_legacy(float, float) __asm("llvm.amdgcn.fmul.legacy");  // v_mul_legacy_f32
 
 namespace sb {
 namespace {
@@ -61,6 +64,13 @@ __device__ inline void wave_sync() {
 }
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The product, 0 where a factor is: z is -inf for an excluded class, which adds nothing
+// to the loss unless it is a target.
+__device__ inline float product(float x, float z) { return sb_mul_legacy(x, z); }
+// Of a row's sum of exponentials, 0 only where every class is excluded.
+__device__ inline float inverse(float s) { return s > 0.0f ? 1.0f / s : 0.0f; }
+__device__ inline float log_of(float s) { return s > 0.0f ? logf(s) : 0.0f; }
 
 // A list place: class and value; unused ones have class -1 and a value of -inf,
 // whatever they held.
@@ -281,6 +291,7 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
       m = wt.max_of(0);
       vm = wt.max_of(1);
     }
+    m = fmaxf(m, -FLT_MAX);  // a row of -inf has z = -inf, not differences of infinities
     float s1 = 0.0f, sT = 0.0f;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
@@ -307,12 +318,11 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
     auto add = [&](const Place& p, float score_c) {
       const float e = place_exp(r, p.v, vm, us);
       zs += e;
-      if (p.id >= 0) ds = fmaf(e, score_c - m, ds);
+      if (p.id >= 0) ds += product(e, score_c - m);
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
       if (s0 + u * step < K) add(now[u], xc[u]);
-#pragma unroll 4
     for (int sl = s0 + AHEAD * step; sl < K; sl += step) {
       const Place p = usable(a, load_place(a, sl, row));
       add(p, score(p.id));
@@ -341,8 +351,8 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
       if (!MIX) s1 = sT;
       const Teacher te = teacher_of(r, zs, us);
       const float A = y >= 0 ? r.w : 0.0f;
-      const float dot = fmaf(te.wt, ds, y >= 0 ? A * (xy - m) : 0.0f);
-      if (hb == 0) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
+      const float dot = product(te.wt, ds) + (y >= 0 ? product(A, xy - m) : 0.0f);
+      if (hb == 0) a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT)) - dot;
     }
     base = nbase;
     loc = nloc;
@@ -418,6 +428,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     } else {
       wave_sync();
     }
+    m = fmaxf(m, -FLT_MAX);
     float zs = 0.0f, us = 0.0f, s1 = 0.0f, sT = 0.0f;
     for (int sl = s0; sl < K; sl += W * PARTS) {
       const float e = place_exp(r, ent[sl * ROWS + rl].e, vm, us);
@@ -458,7 +469,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
     if (!MIX) s1 = sT;
     const Teacher te = teacher_of(r, zs, us);
     const float BQ = r.b * te.Q;
-    const float iT = 1.0f / sT, i1 = 1.0f / s1;
+    const float iT = inverse(sT), i1 = inverse(s1);
     const float kT = (MIX ? BQ : A + BQ) * iT, k1 = A * i1;          // coefficients of the exponentials in g
     const float hT = MIX ? BQ * r.inv_t : A + BQ * r.inv_t, h1 = A;  // of p (1 - p) in h
 
@@ -506,8 +517,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
               e1 = exp2_hw(z * LOG2E);
               gr = fmaf(k1, e1, gr);
             }
-            dot = fmaf(tv[u], z, dot);
-            // columns past the last repeat it: same address, same value, but no target there
+            dot += product(tv[u], z);
             if (live) store_at(Gc, wt.at(i, loc, ld_g), gr);
             if (MODE == 2) {
               const float pT = eT * iT;
@@ -554,7 +564,7 @@ __device__ __forceinline__ void distill_wave(const RowArgs& r, char* lds, int w,
       if (w == 0 && hb == 0) {
         if (a.loss) {
           if (W > 1) dot = wt.sum_of(6);
-          a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
+          a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT)) - dot;
         }
         if (MODE == 2 && a.h_row) {
           if (W > 1) hsum = wt.sum_of(7);
@@ -683,19 +693,19 @@ __global__ void __launch_bounds__(256) k_loss_by_lane(RowArgs r) {
     for (int u = 0; u < 8; ++u) {
       const float e = place_exp(r, p[u].v, vm, us);
       zs += e;
-      ds = fmaf(e, xc[u] - m, ds);
+      ds += product(e, xc[u] - m);
     }
   }
   const Teacher te = teacher_of(r, zs, us);
-  float dot = te.wt * ds, A = 0.0f;
+  float dot = product(te.wt, ds), A = 0.0f;
   if (a.w > 0.0) {
     const int y = a.labels[row];
     if (y >= 0 && y < a.d) {
       A = r.w;
-      dot = fmaf(A, F[(int64_t)y * a.ld_f + loc] - m, dot);
+      dot += product(A, F[(int64_t)y * a.ld_f + loc] - m);
     }
   }
-  if (lane <= left) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - dot;
+  if (lane <= left) a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT)) - dot;
 }
 
 // ---------------------------------------------------------------- wider rows
@@ -722,7 +732,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, in
   const int loc = lane < left ? lane : (int)left;
   const int per = r.cols / WIDE_WAVES, j0 = range * r.cols + w * per;
   const int j1 = j0 + per < a.d ? j0 + per : a.d;
-  float m = -INFINITY, s1 = 0.0f, sT = 0.0f;
+  float m = -FLT_MAX, s1 = 0.0f, sT = 0.0f;
   // two sets of registers in turn: one is read while the other is summed
   float x[2][16];
   auto load = [&](float (&to)[16], int j) {
@@ -762,7 +772,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, in
   sT = s1 = 0.0f;
 #pragma unroll
   for (int u = 0; u < WIDE_WAVES; ++u) {
-    const float z = red[0][u][lane] - mm;  // -inf for a wave without columns, whose sums are 0
+    const float z = red[0][u][lane] - mm;
     sT += red[1][u][lane] * exp2_hw(z * r.c2);
     if (MIX) s1 += red[2][u][lane] * exp2_hw(z * LOG2E);
   }
@@ -838,21 +848,20 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
   }
   const float A = y >= 0 ? r.w : 0.0f;
   float dot = 0.0f, unused = 0.0f;
-#pragma unroll 4
   for (int s = w; s < K; s += WIDE_WAVES) {
     const Place p = usable(a, load_place(a, s, row));
     const float t = te.wt * place_exp(r, p.v, vm, unused);
     if (a.G) targets[s * a.n] = t;
-    if (a.loss && p.id >= 0) dot += t * (a.F[(int64_t)p.id * a.ld_f + row] - m);
+    if (a.loss && p.id >= 0) dot += product(t, a.F[(int64_t)p.id * a.ld_f + row] - m);
   }
   if (a.loss) {
-    if (w == 0 && y >= 0) dot += A * (a.F[(int64_t)y * a.ld_f + row] - m);
+    if (w == 0 && y >= 0) dot += product(A, a.F[(int64_t)y * a.ld_f + row] - m);
     red[0][w][lane] = dot;  // the maxima are read before the barrier above
     __syncthreads();
-    if (w == 0) a.loss[row] = A * logf(s1) + r.bt * (te.ent + te.Q * logf(sT)) - sum_of(0);
+    if (w == 0) a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT)) - sum_of(0);
   }
   if (w == 0 && a.G) {
-    const float BQ = r.b * te.Q, iT = 1.0f / sT, i1 = 1.0f / s1;
+    const float BQ = r.b * te.Q, iT = inverse(sT), i1 = inverse(s1);
     float* out = r.row + row;
     out[0] = m;
     out[a.n] = (MIX ? BQ : A + BQ) * iT;

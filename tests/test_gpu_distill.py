@@ -240,6 +240,66 @@ def test_far_scores(d):
         check(F, ids, vals, T, 0.5, y, "logits", *run(F, ids, vals, T, 0.5, y, "logits"))
 
 
+@pytest.mark.parametrize("n,d", [(70, 8), (70, 60), (65, 300), (40, 900), (5, 1600)])
+@pytest.mark.parametrize("T,w", [(1.0, 0.4), (2.0, 0.4), (3.0, 0.0)])
+def test_excluded_classes(n, d, T, w):
+    """A score of -inf is one so low that its probability is 0 in fp64 as well; a target on it makes the loss +inf."""
+    rng = np.random.default_rng(d)
+    F, ids, vals, y = inputs(rng, n, d, 5, "logits")
+    out = rng.random((n, d)) < 0.3
+    for i in range(n):  # no target is excluded, but those of the last rows
+        used = (ids[:, i] >= 0) & (ids[:, i] < d)
+        out[i, ids[used, i]] = False
+        out[i, 0] = False
+        if 0 <= y[i] < d:
+            out[i, y[i]] = False
+    ids[0, n - 3:], vals[0, n - 3:] = d - 1, 1.0
+    out[n - 3:, d - 1] = True
+    out[n - 2] = True  # every class
+    X, low = np.where(out, np.float32(-np.inf), F), np.where(out, np.float32(-1e4), F)
+    fwd, got = run(X, ids, vals, T, w, y, "logits")
+    hit = np.arange(n - 3, n)
+    assert np.all(fwd[hit] == np.inf) and np.all(got["loss"][hit] == np.inf)
+    _, g, h = osc.distill(X[hit], ids[:, hit], vals[:, hit], T, w, y[hit], "logits")
+    # q eps(q) <= u (5 + 16 + 3 * 13), p eps(p) <= u (25 + 16 + 6 * 7) where p is near 1, less for more classes; g adds
+    # them with w and (1 - w) T, h has p eps(p) twice
+    assert np.allclose(got["G"].T[hit], g, rtol=0, atol=256 * U * max(T, 1.0))
+    assert np.allclose(got["hess"].T[hit], h, rtol=0, atol=256 * U)
+    assert not got["hess"][:, n - 2].any() and got["h_row"][n - 2] == 0
+    keep = np.arange(n - 3)
+    check(low, ids, vals, T, w, y, "logits", fwd, got, keep)
+
+
+@pytest.mark.parametrize("d", [30, 400])
+def test_excluded_classes_in_many_rows(d):
+    rng = np.random.default_rng(d)
+    n, k = 100_003, 1
+    F = rng.normal(size=(n, d)).astype(np.float32)
+    ids, vals = rng.integers(0, d // 2, (k, n)).astype(np.int32), rng.normal(size=(k, n)).astype(np.float32)
+    ids[0, n - 1] = d - 1
+    low = F.copy()
+    low[:, d // 2:] = -1e4
+    F[:, d // 2:] = -np.inf
+    F[n - 2] = -np.inf
+    ids[0, n - 2] = -1
+    fwd, got = run(F, ids, vals, 2.0, 0.0, None, "logits")
+    assert fwd[n - 1] == np.inf and fwd[n - 2] == 0 and got["loss"][n - 1] == np.inf and got["loss"][n - 2] == 0
+    check(low, ids, vals, 2.0, 0.0, None, "logits", fwd, got, np.concatenate([np.arange(200), np.arange(n - 70, n - 2)]))
+
+
+@pytest.mark.parametrize("d", [5, 100, 700, 1600])
+def test_nan_and_inf_stay_in_their_row(d):
+    rng = np.random.default_rng(d)
+    F, ids, vals, y = inputs(rng, 70, d, 5, "logits")
+    _, want = run(F, ids, vals, 2.0, 0.3, y, "logits", norms=False)
+    bad = F.copy()
+    bad[3, 0], bad[64, d - 1], bad[69, 2] = np.nan, np.inf, np.nan
+    fwd, got = run(bad, ids, vals, 2.0, 0.3, y, "logits", norms=False)
+    keep = np.setdiff1d(np.arange(70), [3, 64, 69])
+    for name in want:
+        assert np.array_equal(got[name][..., keep], want[name][..., keep]), name
+
+
 @pytest.mark.parametrize("d", [12, 100, 700, 1600])
 def test_outputs_are_optional(d):
     rng = np.random.default_rng(d)

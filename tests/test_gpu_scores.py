@@ -151,6 +151,53 @@ def test_many_rows(order, dtype, n, d, k):
 
 # Leading dimensions past the matrix (the gaps hold NaN), matrices that start off a vector's alignment, lists with a
 # leading dimension of their own.
+# Several rows per wave and block in turn, at each width of a row's threads: 2048 blocks of four waves up to 1024 and
+# 4096 classes, 1024 up to 16384, 512 or 256 beyond.  Every third row holds few different scores, so that its
+# candidates outnumber their places, next to rows whose do not.
+@pytest.mark.parametrize("dtype", ["f32", "f16", "bf16"])
+@pytest.mark.parametrize("n,d,k", [(9001, 700, 10), (9003, 100, 33), (8200, 641, 64), (2050, 1025, 12), (8300, 1100, 40),
+                                   (1100, 4097, 5), (1040, 4500, 64), (515, 16_385, 20), (600, 16_390, 64),
+                                   (300, 20_001, 33), (520, 5000, 0)])
+def test_rows_in_turn(dtype, n, d, k):
+    print("case: log_probs row", dtype, n, d, k, flush=True)
+    rng = np.random.default_rng(n + d + k)
+    F = rng.normal(size=(n, d)).astype(np.float32) * 3
+    F[::3] = rng.integers(0, 3, F[::3].shape)
+    F = rounded(F, dtype)
+    y = labels_of(rng, n, d)
+    rows = np.unique(np.concatenate([np.arange(6), np.arange(n - 6, n), rng.integers(0, n, 60)]))
+    check(F, run(F, "row", dtype, 2.0, y, k), 2.0, y, k, rows)
+
+
+# Lists of every length class and both sides of the rules that choose lanes, waves, and the column splits and how many
+# lanes join them.
+@pytest.mark.parametrize("order,n,d,k", [("row", 160 * 40 - 1, 40, 5), ("row", 160 * 40, 40, 5), ("row", 102_400, 640, 3),
+                                         ("row", 102_560, 641, 3), ("row", 20_000, 90, 14), ("row", 20_000, 90, 17),
+                                         ("row", 20_000, 90, 48), ("row", 20_000, 90, 1), ("row", 20_000, 90, 0),
+                                         ("col", 5000, 8 * 64 - 1, 9), ("col", 5000, 8 * 64, 13), ("col", 1000, 9 * 64, 20),
+                                         ("col", 1000, 16 * 64, 64), ("col", 700, 17 * 64, 12), ("col", 64, 64 * 64, 33),
+                                         ("col", 64, 65_535, 64), ("col", 60_000, 130, 33), ("col", 60_000, 130, 32),
+                                         ("col", 43_000, 200, 64), ("col", 131_009, 130, 16), ("col", 131_073, 130, 16)])
+def test_both_sides_of_the_rules(order, n, d, k):
+    print("case: log_probs", order, n, d, k, flush=True)
+    rng = np.random.default_rng(n + d + k)
+    F = rng.normal(size=(n, d)).astype(np.float32)
+    F[1::2] = np.round(F[1::2])
+    y = labels_of(rng, n, d)
+    rows = np.unique(np.concatenate([np.arange(6), np.arange(n - 6, n), rng.integers(0, n, 150)]))
+    check(F, run(F, order, "f32", 0.7, y, k), 0.7, y, k, rows)
+
+
+# Scores in ascending order make every class enter the list, in descending order only the first ones.
+@pytest.mark.parametrize("order,dtype", CASES)
+@pytest.mark.parametrize("n,d,k", [(70, 300, 20), (20_000, 100, 64), (20_000, 100, 10), (40, 3000, 64)])
+@pytest.mark.parametrize("up", [True, False])
+def test_sorted_scores(order, dtype, n, d, k, up):
+    F = rounded(np.tile(np.arange(d, dtype=np.float32) * (0.25 if up else -0.25), (n, 1)), dtype)
+    rows = np.array([0, 1, 63, n - 2, n - 1]) % n
+    check(F, run(F, order, dtype, 1.0, None, k), 1.0, None, k, rows)
+
+
 @pytest.mark.parametrize("order,dtype", CASES)
 @pytest.mark.parametrize("n,d,pad,shift", [(70, 50, 1, 0), (70, 50, 3, 1), (33, 1001, 5, 3), (5, 9001, 7, 5), (130, 8, 8, 7),
                                            (1, 2051, 13, 1), (3, 40_003, 2, 6)])
