@@ -112,14 +112,16 @@ __device__ inline int wave_sum(int x) {
 // -inf has s = 0 and no differences of infinities.
 struct RowStats {
   float m, s, t;
-  __device__ float log_s() const { return logf(s); }
+  float r;  // s and t are those of y_j + r (see rows_in_block); 0 elsewhere
+  __device__ float log_s() const { return logf(s) - LN2 * r; }
 };
 __device__ inline void store_row(const LogProbArgs& a, int64_t row, const RowStats& r, int y, float ay, int before) {
   const float ls = r.log_s();
   const bool none = r.s == 0.0f;
   const bool has = y >= 0 && y < a.d;
   if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(r.m, a.c, ls);
-  if (a.entropy) a.entropy[row] = none ? 0.0f : ls - LN2 * r.t / r.s;
+  const float h = ls - LN2 * (r.t / r.s - r.r);
+  if (a.entropy) a.entropy[row] = none || h < 0.0f ? 0.0f : h;
   if (a.logp) a.logp[row] = !has ? 0.0f : none ? -INFINITY : (ay - r.m) * a.c - ls;
   if (a.rank) a.rank[row] = has ? before : -1;
 }
@@ -315,7 +317,7 @@ struct LaneRow {
 template <int KM>
 __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t row, int split, int y, float ay) {
   if (a.splits == 1) {
-    const RowStats st{r.m, r.s, r.t};
+    const RowStats st{r.m, r.s, r.t, 0.0f};
     store_row(a, row, st, y, ay, r.before);
     const float ls = st.log_s();
 #pragma unroll
@@ -520,7 +522,7 @@ __global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
   const float s = group_all<G>(f * ms.y, add, fdpp);
   const float t = group_all<G>(f * fmaf(ms.y, dy, tb.x), add, fdpp);
   const int before = group_all<G>(__float_as_int(tb.y), add, idpp);
-  const RowStats st{mm, s, t};
+  const RowStats st{mm, s, t, 0.0f};
   const int y = a.labels ? a.labels[row] : -1;
   if (lane == 0) {
     const float ay = y >= 0 && y < a.d ? static_cast<const float*>(a.F)[(int64_t)y * a.ld + row] : 0.0f;
@@ -642,26 +644,39 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     if (j < whole) __builtin_memcpy(&v, F + j, 16);
     return v;
   };
-  // 16-bit scores stay as they are and are widened where they are used
+  // Scores stay as they are in memory until they are used: a conversion here would wait
+  // for them.  The given class is known a row ahead, so its score is read with the row.
   u32x4 raw[NV];
-  float tail, ay;
-  int y;
+  T tail_raw, ay_raw, mates_raw;  // mates: those before the given class in its 16 bytes, one per thread
+  int y = -1, y_next = -1;
+  int lane_0 = 0;
+  asm("" : "+v"(lane_0));  // labels in vector registers: moved to scalar ones, they would be waited for
   auto load_scalars = [&](int64_t r) {
-    const T* F = row_at(r);
-    tail = whole + tid < a.d ? to_f32(F[whole + tid]) : -INFINITY;
-    y = a.labels ? a.labels[r] : -1;
-    ay = y >= 0 && y < a.d ? to_f32(F[y]) : 0.0f;
+    const T* F = row_at(r < a.n ? r : a.n - 1);
+    int tail_at = whole + tid < a.d ? whole + tid : 0, at = y >= 0 && y < a.d ? y : 0;
+    int mate_at = at - min(at & (VEC - 1), tid + 1);
+    asm("" : "+v"(tail_at), "+v"(at), "+v"(mate_at));  // indices, not branches
+    tail_raw = F[tail_at];
+    ay_raw = F[at];
+    mates_raw = F[mate_at];
+  };
+  auto load_label = [&](int64_t r) {
+    if (a.labels) y_next = (a.labels + (r < a.n ? r : a.n - 1))[lane_0];
   };
 #pragma unroll
   for (int q = 0; q < NV; ++q)
     if (q * NT * VEC < whole) raw[q] = load_vec(row_at(row), q);
+  load_label(row);
+  y = y_next;
   load_scalars(row);
+  load_label(row + stride);
   if (tid == 0) sh.pieces[0] = sh.count[0] = 0;
   for (int turn = 0; row < a.n; row += stride, turn ^= 1) {
     // the compiler sees the thread anew in every row: the places of its scores, a
     // register each, would otherwise be held across the rows
     asm volatile("" : "+v"(tid));
     // the maxima of the even vectors and of the odd ones
+    const float tail = whole + tid < a.d ? to_f32(tail_raw) : -INFINITY;
     float lm[2] = {tail, -INFINITY};
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
@@ -672,6 +687,13 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       for (int u = 0; u < VEC; ++u) lm[q & 1] = fmaxf(lm[q & 1], x[u]);
       asm volatile("" : "+v"(lm[q & 1]));
     }
+    // the row is here; told so, the compiler waits for nothing among the sums below, where
+    // the next one's scores are on their way
+    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    const int64_t next_row = row + stride;
+    const int y_now = y;
+    const float ay = y >= 0 && y < a.d ? to_f32(ay_raw) : 0.0f;
+    const bool mate = y >= 0 && y < whole && tid < (y & (VEC - 1)) && to_f32(mates_raw) == ay;
     if (W > 1) {
       sh.lane_max[0][w][lane] = lm[0];
       sh.lane_max[1][w][lane] = lm[1];
@@ -693,10 +715,14 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       // -inf is no candidate; the lowest score above it is -FLT_MAX
       b = kb > KEY_EXCLUDED ? key_score(kb) : -FLT_MAX;
     }
+    // y_j + r in one rounding: a_j c2 - m2 for the rounded m2 = m c2, where its error r is small
+    const float m2 = m * a.c2;
+    const bool far = !(fabsf(m2) < 0x1p20f);
+    const float r = far ? 0.0f : fmaf(m, a.c2, -m2);
     float s = 0.0f, t = 0.0f;
     int before = 0;
-    auto add = [&](float xv) {
-      const float yv = (xv - m) * a.c2, e = exp2_hw(yv);
+    auto term = [&](float yv) {
+      const float e = exp2_hw(yv);
       s += e;
       t = fmaf(e, fmaxf(yv, -1500.0f), t);
     };
@@ -706,8 +732,8 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
         if (at < CAP) sh.cand[at] = cand_of(xv, j);
       }
     };
-    add(tail);
-    if (a.rank) before = tail > ay || (tail == ay && whole + tid < y);
+    term(fmaf(tail, a.c2, -m2));
+    if (a.rank) before = (tail > ay || (tail == ay && whole + tid < y_now)) + mate;
     if (a.k > 0) collect(tail, whole + tid);
     const float ay_below = below(ay);
 #pragma unroll
@@ -717,17 +743,13 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       decode<T>(raw[q], x);
       const int j = (q * NT + tid) * VEC;
 #pragma unroll
-      for (int u = 0; u < VEC; ++u) add(x[u]);
+      for (int u = 0; u < VEC; ++u) term(fmaf(x[u], a.c2, -m2));
       asm volatile("" : "+v"(s), "+v"(t));  // here and now: put off, the terms take more registers than there are
       if (a.rank) {
-        // classes before y come first at equal scores; y's own vector is all "behind" it, but for its equals
-        const float over = j + VEC <= y ? ay_below : ay;
+        // classes before y come first at equal scores; those in its own 16 bytes are mates
+        const float over = j + VEC <= y_now ? ay_below : ay;
 #pragma unroll
         for (int u = 0; u < VEC; ++u) before += !(x[u] <= over);
-        if (j <= y && y < j + VEC) {
-#pragma unroll
-          for (int u = 0; u < VEC; ++u) before += x[u] == ay && j + u < y;
-        }
         asm volatile("" : "+v"(before));
       }
       if (a.k > 0) {
@@ -742,17 +764,14 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
           }
         }
       }
+      if (next_row < a.n) raw[q] = load_vec(row_at(next_row), q);
     }
-    // the registers are free: the next row's scores are on their way through what
-    // follows (among the sums above, each would be waited for at the next vector)
-    const int y_now = y;
-    const float ay_now = ay;
-    if (row + stride < a.n) {
-      const T* next = row_at(row + stride);
-#pragma unroll
-      for (int q = 0; q < NV; ++q)
-        if (q * NT * VEC < whole) raw[q] = load_vec(next, q);
-      load_scalars(row + stride);
+    y = y_next;
+    load_scalars(next_row);
+    load_label(next_row + stride);
+    if (far) {  // scores of such size: differences first, from memory once more
+      s = t = 0.0f;
+      for (int j = tid; j < a.d; j += NT) term((to_f32(row_at(row)[j]) - m) * a.c2);
     }
     s = wave_sum(s);
     t = wave_sum(t);
@@ -773,8 +792,8 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
         before += __float_as_int(sh.sums[2][u]);
       }
     }
-    const RowStats st{m, s, t};
-    if (tid == 0) store_row(a, row, st, y_now, ay_now, before);
+    const RowStats st{m, s, t, r};
+    if (tid == 0) store_row(a, row, st, y_now, ay, before);
     if (a.k == 0) continue;
     const int pieces = sh.pieces[turn];
     for (int i = tid; i < (pieces < CAP / 2 ? pieces : CAP / 2) * VEC; i += NT) {
@@ -824,7 +843,7 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
 
 // A block of 256 has four rows of a wave each, or one row.
 template <typename T, int NT, int E>
-__global__ void __launch_bounds__(NT == 64 ? 256 : NT) k_row_in_block(LogProbArgs a) {
+__global__ void __launch_bounds__(NT == 64 ? 256 : NT, 4) k_row_in_block(LogProbArgs a) {
   constexpr int ROWS = NT == 64 ? 4 : 1;
   __shared__ RowShared<NT> sh[ROWS];
   const int rg = NT == 64 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
@@ -920,8 +939,11 @@ int32_t launch_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n,
     a.ld = d;
   }
   if (order == SB_COLUMN_MAJOR) {
+    // whole steps, so that none but the row's end is filled up: a filled column is an
+    // excluded class, which would count among those before an excluded one
     a.splits = column_splits(n, d, k);
-    a.per = (d + a.splits - 1) / a.splits;
+    a.per = ((d + a.splits - 1) / a.splits + CH - 1) / CH * CH;
+    a.splits = (d + a.per - 1) / a.per;
     a.part = static_cast<double*>(ws);
     const int64_t units = (int64_t)a.tiles * a.splits;
     by_list<ColsByLane>(k, a, dim3((unsigned)((units + 3) / 4)), st);
