@@ -113,14 +113,17 @@ __device__ inline int wave_sum(int x) {
 struct RowStats {
   float m, s, t;
   float r;  // s and t are those of y_j + r (see rows_in_block); 0 elsewhere
-  __device__ float log_s() const { return logf(s) - LN2 * r; }
+  // in powers of 2 by the hardware's logarithm: s is near 1 or above, or 0
+  __device__ float log2_s() const { return __builtin_amdgcn_logf(s); }
+  __device__ float log_s(float l2) const { return LN2 * (l2 - r); }
+  __device__ float entropy(float l2) const { return LN2 * (l2 - t * __builtin_amdgcn_rcpf(s)); }
 };
-__device__ inline void store_row(const LogProbArgs& a, int64_t row, const RowStats& r, int y, float ay, int before) {
-  const float ls = r.log_s();
+// ls: log s; h: the entropy
+__device__ inline void store_row(const LogProbArgs& a, int64_t row, const RowStats& r, float ls, float h, int y, float ay,
+                                 int before) {
   const bool none = r.s == 0.0f;
   const bool has = y >= 0 && y < a.d;
   if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(r.m, a.c, ls);
-  const float h = ls - LN2 * (r.t / r.s - r.r);
   if (a.entropy) a.entropy[row] = none || h < 0.0f ? 0.0f : h;
   if (a.logp) a.logp[row] = !has ? 0.0f : none ? -INFINITY : (ay - r.m) * a.c - ls;
   if (a.rank) a.rank[row] = has ? before : -1;
@@ -318,8 +321,8 @@ template <int KM>
 __device__ inline void finish_lane(const LogProbArgs& a, LaneRow<KM>& r, int64_t row, int split, int y, float ay) {
   if (a.splits == 1) {
     const RowStats st{r.m, r.s, r.t, 0.0f};
-    store_row(a, row, st, y, ay, r.before);
-    const float ls = st.log_s();
+    const float l2 = st.log2_s(), ls = st.log_s(l2);
+    store_row(a, row, st, ls, st.entropy(l2), y, ay, r.before);
 #pragma unroll
     for (int q = 0; q < KM; ++q) {
       const int at = r.place_in(q, a.k);
@@ -523,13 +526,13 @@ __global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
   const float t = group_all<G>(f * fmaf(ms.y, dy, tb.x), add, fdpp);
   const int before = group_all<G>(__float_as_int(tb.y), add, idpp);
   const RowStats st{mm, s, t, 0.0f};
+  const float l2 = st.log2_s(), ls = st.log_s(l2);
   const int y = a.labels ? a.labels[row] : -1;
   if (lane == 0) {
     const float ay = y >= 0 && y < a.d ? static_cast<const float*>(a.F)[(int64_t)y * a.ld + row] : 0.0f;
-    store_row(a, row, st, y, ay, before);
+    store_row(a, row, st, ls, st.entropy(l2), y, ay, before);
   }
   if (a.k == 0) return;
-  const float ls = st.log_s();
   list += 2 * a.n;
   auto place = [&](int at) { return on && at < a.k ? list[(int64_t)at * a.n] : -INFINITY; };
   int at = 2;
@@ -565,6 +568,7 @@ constexpr uint32_t KEY_EXCLUDED = 0x007fffffu;  // of -inf
 template <int NT>
 struct RowShared {
   static constexpr int W = NT / 64, CAP = NT == 64 ? CAND_WAVE : CAND_BLOCK;
+  static_assert(CAP % 8 == 0, "places are read eight at a time");
   u32x4 piece[CAP / 2];
   uint64_t cand[CAP];
   uint64_t best[SB_MAX_TOP];
@@ -618,7 +622,13 @@ __device__ inline void ranked(const RowShared<NT>& sh, int found, int k, int tid
 #pragma unroll
       for (int u = 0; u < 8; ++u) place += c[u] > mine;
     }
-    for (; o < found; ++o) place += sh.cand[o] > mine;
+    if (o < found) {  // the rest, as many read at once
+      uint64_t c[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) c[u] = sh.cand[o + u];
+#pragma unroll
+      for (int u = 0; u < 7; ++u) place += o + u < found && c[u] > mine;
+    }
     if (place < k) put(place, mine);
   }
 }
@@ -726,11 +736,24 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       s += e;
       t = fmaf(e, fmaxf(yv, -1500.0f), t);
     };
-    auto collect = [&](float xv, int j) {
-      if (xv >= b) {
-        const int at = atomicAdd(&sh.count[turn], 1);
-        if (at < CAP) sh.cand[at] = cand_of(xv, j);
+    // the next of a row's numbers for every thread that wants one: a wave alone counts by itself
+    int own_pieces = 0, own_count = 0;
+    auto number = [&](bool want, int& own, int* shared) {
+      const uint64_t all = __ballot(want);
+      int at = own;
+      if constexpr (W > 1) {
+        int first = 0;
+        if (all && lane == 0) first = atomicAdd(shared, __popcll(all));
+        at = __builtin_amdgcn_readfirstlane(first);
+      } else {
+        own += __popcll(all);
       }
+      return at + (int)__builtin_amdgcn_mbcnt_hi((uint32_t)(all >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)all, 0));
+    };
+    auto collect = [&](float xv, int j) {
+      if (!__any(xv >= b)) return;
+      const int at = number(xv >= b, own_count, &sh.count[turn]);
+      if (xv >= b && at < CAP) sh.cand[at] = cand_of(xv, j);
     };
     term(fmaf(tail, a.c2, -m2));
     if (a.rank) before = (tail > ay || (tail == ay && whole + tid < y_now)) + mate;
@@ -756,9 +779,9 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
         float xm = x[0];
 #pragma unroll
         for (int u = 1; u < VEC; ++u) xm = fmaxf(xm, x[u]);
-        if (xm >= b) {  // the 16 bytes that hold a candidate
-          const int at = atomicAdd(&sh.pieces[turn], 1);
-          if (at < CAP / 2) {
+        if (__any(xm >= b)) {  // the 16 bytes that hold a candidate
+          const int at = number(xm >= b, own_pieces, &sh.pieces[turn]);
+          if (xm >= b && at < CAP / 2) {
             sh.piece[at] = raw[q];
             sh.piece_at[at] = j;
           }
@@ -793,16 +816,18 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       }
     }
     const RowStats st{m, s, t, r};
-    if (tid == 0) store_row(a, row, st, y_now, ay, before);
+    const float l2 = st.log2_s(), ls = st.log_s(l2);
+    if (tid == 0) store_row(a, row, st, ls, st.entropy(l2), y_now, ay, before);
     if (a.k == 0) continue;
-    const int pieces = sh.pieces[turn];
-    for (int i = tid; i < (pieces < CAP / 2 ? pieces : CAP / 2) * VEC; i += NT) {
-      const T* e = reinterpret_cast<const T*>(&sh.piece[i / VEC]);
-      collect(to_f32(e[i % VEC]), sh.piece_at[i / VEC] + i % VEC);
+    const int pieces = W > 1 ? sh.pieces[turn] : own_pieces;
+    const int parts = (pieces < CAP / 2 ? pieces : CAP / 2) * VEC;
+    for (int i0 = 0; i0 < parts; i0 += NT) {
+      const uint32_t i = i0 + tid, at = (int)i < parts ? i : 0;
+      const float v = to_f32(reinterpret_cast<const T*>(sh.piece)[at]);
+      collect((int)i < parts ? v : -INFINITY, sh.piece_at[at / VEC] + (int)(at % VEC));
     }
     sync();  // 3
-    int found = sh.count[turn];
-    const float ls = st.log_s();
+    int found = W > 1 ? sh.count[turn] : own_count;
     if (pieces <= CAP / 2 && found <= CAP) {
       ranked<NT>(sh, found, a.k, tid,
                  [&](int place, uint64_t c) { store_top(a, row, place, cand_score(c), cand_class(c), st, ls); });
