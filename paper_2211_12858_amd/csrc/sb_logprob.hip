@@ -23,6 +23,7 @@
 
 #include <cfloat>
 #include <cmath>
+#include <type_traits>
 
 #include "sb_common.h"
 
@@ -55,15 +56,42 @@ __device__ inline float to_f32(float x) { return x; }
 __device__ inline float to_f32(__half x) { return __half2float(x); }
 __device__ inline float to_f32(__hip_bfloat16 x) { return __bfloat162float(x); }
 // The scores in 16 bytes, and 16 bytes of excluded ones.  The compiler sees the bytes
-// anew: it would otherwise widen once and keep both forms.
+// anew: it would otherwise widen once and keep both forms.  fp16 ones are compared as
+// they are, and widened by the instruction that scales them.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <typename T>
-__device__ inline void decode(u32x4& raw, float (&x)[16 / sizeof(T)]) {
+using Score = std::conditional_t<std::is_same_v<T, __half>, _Float16, float>;
+template <typename T>
+__device__ inline void decode(u32x4& raw, Score<T> (&x)[16 / sizeof(T)]) {
   asm volatile("" : "+v"(raw));
-  T e[16 / sizeof(T)];
-  __builtin_memcpy(e, &raw, 16);
+  if constexpr (std::is_same_v<T, __half>) {
+    __builtin_memcpy(x, &raw, 16);
+  } else {
+    T e[16 / sizeof(T)];
+    __builtin_memcpy(e, &raw, 16);
 #pragma unroll
-  for (int u = 0; u < (int)(16 / sizeof(T)); ++u) x[u] = to_f32(e[u]);
+    for (int u = 0; u < (int)(16 / sizeof(T)); ++u) x[u] = to_f32(e[u]);
+  }
+}
+// Their maximum (of numbers).
+__device__ inline float max_of(const u32x4& raw, const _Float16 (&)[8]) {
+  uint32_t a, b;
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(a) : "v"(raw.x), "v"(raw.y));
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(b) : "v"(raw.z), "v"(raw.w));
+  asm("v_pk_max_f16 %0, %0, %1" : "+v"(a) : "v"(b));
+  _Float16 h[2];
+  __builtin_memcpy(h, &a, 4);
+  return fmaxf((float)h[0], (float)h[1]);
+}
+template <int N>
+__device__ inline float max_of(const u32x4&, const float (&x)[N]) {
+  float m = x[N - 1];
+#pragma unroll
+  for (int u = 0; u + 1 < N; u += 2) {  // as it stands: the compiler would round bf16 maxima to bf16 again
+    if (u + 2 < N) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m) : "v"(x[u]), "v"(x[u + 1]));
+    else asm("v_max_f32 %0, %0, %1" : "+v"(m) : "v"(x[u]));
+  }
+  return m;
 }
 __device__ inline uint32_t excluded(float) { return 0xff800000u; }
 __device__ inline uint32_t excluded(__half) { return 0xfc00fc00u; }
@@ -599,13 +627,16 @@ __device__ inline uint32_t key_bound(uint32_t k0, uint32_t k1, int k) {
   return bound;
 }
 
-// The largest float below v, so that x >= v is x > below(v); NaN below -inf, which
+// The largest score below v, so that x >= v is x > below(v); NaN below -inf, which
 // nothing is "not above".
 __device__ inline float below(float v) {
-  if (v == -INFINITY) return NAN;
   const uint32_t b = __float_as_uint(v + 0.0f);
-  if (b == 0) return __uint_as_float(0x80000001u);
-  return __uint_as_float(v > 0.0f ? b - 1 : b + 1);
+  return v == -INFINITY ? NAN : __uint_as_float(b == 0 ? 0x80000001u : v > 0.0f ? b - 1 : b + 1);
+}
+__device__ inline _Float16 below(_Float16 v) {
+  const uint16_t b = __builtin_bit_cast(uint16_t, v);
+  const uint16_t to = (b & 0x7fff) == 0 ? 0x8001 : (b & 0x8000) == 0 ? b - 1 : b + 1;
+  return __builtin_bit_cast(_Float16, (uint16_t)(b == 0xfc00 ? 0x7e00 : to));
 }
 
 // put(place, candidate) for the k best of the first `found` candidates: a candidate's
@@ -691,10 +722,9 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       if (q * NT * VEC >= whole) continue;
-      float x[VEC];
+      Score<T> x[VEC];
       decode<T>(raw[q], x);
-#pragma unroll
-      for (int u = 0; u < VEC; ++u) lm[q & 1] = fmaxf(lm[q & 1], x[u]);
+      lm[q & 1] = fmaxf(lm[q & 1], max_of(raw[q], x));
       asm volatile("" : "+v"(lm[q & 1]));
     }
     // the row is here; told so, the compiler waits for nothing among the sums below, where
@@ -758,27 +788,25 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     term(fmaf(tail, a.c2, -m2));
     if (a.rank) before = (tail > ay || (tail == ay && whole + tid < y_now)) + mate;
     if (a.k > 0) collect(tail, whole + tid);
-    const float ay_below = below(ay);
+    const Score<T> ay_below = below((Score<T>)ay);
 #pragma unroll
     for (int q = 0; q < NV; ++q) {
       if (q * NT * VEC >= whole) continue;
-      float x[VEC];
+      Score<T> x[VEC];
       decode<T>(raw[q], x);
       const int j = (q * NT + tid) * VEC;
 #pragma unroll
-      for (int u = 0; u < VEC; ++u) term(fmaf(x[u], a.c2, -m2));
+      for (int u = 0; u < VEC; ++u) term(fmaf((float)x[u], a.c2, -m2));
       asm volatile("" : "+v"(s), "+v"(t));  // here and now: put off, the terms take more registers than there are
       if (a.rank) {
         // classes before y come first at equal scores; those in its own 16 bytes are mates
-        const float over = j + VEC <= y_now ? ay_below : ay;
+        const Score<T> over = j + VEC <= y_now ? ay_below : (Score<T>)ay;
 #pragma unroll
         for (int u = 0; u < VEC; ++u) before += !(x[u] <= over);
         asm volatile("" : "+v"(before));
       }
       if (a.k > 0) {
-        float xm = x[0];
-#pragma unroll
-        for (int u = 1; u < VEC; ++u) xm = fmaxf(xm, x[u]);
+        const float xm = max_of(raw[q], x);
         if (__any(xm >= b)) {  // the 16 bytes that hold a candidate
           const int at = number(xm >= b, own_pieces, &sh.pieces[turn]);
           if (xm >= b && at < CAP / 2) {
