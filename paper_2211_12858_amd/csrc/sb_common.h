@@ -42,6 +42,11 @@ __device__ inline void lds_barrier() {
   asm volatile("" ::: "memory");
 }
 
+// Waits for all of this wave's global loads and stores.  Before a load in a branch it
+// tells the compiler that earlier ones have come: where the branches meet again it
+// would wait for them by counting, and then for the branch's own load as well.
+__device__ inline void wait_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+
 // A 32-bit value moved across lanes by a DPP control (row shift or row
 // broadcast); lanes the control does not write get `old`.
 template <int CTRL, int ROW_MASK>

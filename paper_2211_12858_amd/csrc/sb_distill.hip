@@ -659,9 +659,11 @@ __global__ void __launch_bounds__(256) k_loss_by_lane(RowArgs r) {
   };
   load(x[0], 0);
   for (int j = 0; j < a.d; j += 32) {
+    wait_loads();
     if (j + 16 < a.d) load(x[1], j + 16);
     step(x[0]);
     if (j + 16 < a.d) {
+      wait_loads();
       if (j + 32 < a.d) load(x[0], j + 32);
       step(x[1]);
     }
@@ -740,6 +742,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, in
     for (int i = 0; i < 16; ++i) to[i] = (a.F + (int64_t)(j + i < j1 ? j + i : j1 - 1) * a.ld_f + base)[loc];
   };
   auto step = [&](const float (&now)[16], float (&next)[16], int j) {
+    wait_loads();
     if (j + 16 < j1) load(next, j + 16);
     float mn = m;
 #pragma unroll
@@ -789,9 +792,9 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, in
 //   row[3] 1 / sT, row[4] 1 / s1, row[5] Q, then the targets of the K places.
 constexpr int ROW_VALUES = 6;
 
-template <bool MIX>
-__global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
-  __shared__ float red[6][WIDE_WAVES][64];
+template <bool MIX, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) k_distill_rows(RowArgs r) {
+  __shared__ float red[6][WAVES][64];
   const DistillArgs& a = r.a;
   const int K = a.k;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -802,20 +805,20 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
   auto sum_of = [&](int q) {
     float s = red[q][0][lane];
 #pragma unroll
-    for (int u = 1; u < WIDE_WAVES; ++u) s += red[q][u][lane];
+    for (int u = 1; u < WAVES; ++u) s += red[q][u][lane];
     return s;
   };
   auto max_of = [&](int q) {
     float s = red[q][0][lane];
 #pragma unroll
-    for (int u = 1; u < WIDE_WAVES; ++u) s = fmaxf(s, red[q][u][lane]);
+    for (int u = 1; u < WAVES; ++u) s = fmaxf(s, red[q][u][lane]);
     return s;
   };
   float m = -INFINITY, vm = -INFINITY;
 #pragma unroll 4
-  for (int q = w; q < r.ranges; q += WIDE_WAVES) m = fmaxf(m, r.stats[(int64_t)q * 3 * a.n + row]);
+  for (int q = w; q < r.ranges; q += WAVES) m = fmaxf(m, r.stats[(int64_t)q * 3 * a.n + row]);
 #pragma unroll 4
-  for (int s = w; s < K; s += WIDE_WAVES) vm = fmaxf(vm, usable(a, load_place(a, s, row)).v);
+  for (int s = w; s < K; s += WAVES) vm = fmaxf(vm, usable(a, load_place(a, s, row)).v);
   red[0][w][lane] = m;
   red[1][w][lane] = vm;
   __syncthreads();
@@ -823,14 +826,14 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
   vm = max_of(1);
   float sT = 0.0f, s1 = 0.0f, zs = 0.0f, us = 0.0f;
 #pragma unroll 4
-  for (int q = w; q < r.ranges; q += WIDE_WAVES) {
+  for (int q = w; q < r.ranges; q += WAVES) {
     const float* st = r.stats + (int64_t)q * 3 * a.n + row;
     const float z = st[0] - m;
     sT = fmaf(st[a.n], exp2_hw(z * r.c2), sT);
     if (MIX) s1 = fmaf(st[2 * a.n], exp2_hw(z * LOG2E), s1);
   }
 #pragma unroll 4
-  for (int s = w; s < K; s += WIDE_WAVES) zs += place_exp(r, usable(a, load_place(a, s, row)).v, vm, us);
+  for (int s = w; s < K; s += WAVES) zs += place_exp(r, usable(a, load_place(a, s, row)).v, vm, us);
   red[2][w][lane] = sT;
   red[3][w][lane] = s1;
   red[4][w][lane] = zs;
@@ -848,7 +851,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_rows(RowArgs r) {
   }
   const float A = y >= 0 ? r.w : 0.0f;
   float dot = 0.0f, unused = 0.0f;
-  for (int s = w; s < K; s += WIDE_WAVES) {
+  for (int s = w; s < K; s += WAVES) {
     const Place p = usable(a, load_place(a, s, row));
     const float t = te.wt * place_exp(r, p.v, vm, unused);
     if (a.G) targets[s * a.n] = t;
@@ -1049,7 +1052,10 @@ void launch_wide(const RowArgs& r, const DistillWidePlan& p, hipStream_t st) {
   const dim3 block(64 * WIDE_WAVES);
   auto blocks = [](int units) { return dim3((units + 7) / 8 * 8); };
   hipLaunchKernelGGL(k_distill_stats<MIX>, blocks(p.ranges * p.tiles), block, 0, st, r, p.ranges * p.tiles);
-  hipLaunchKernelGGL(k_distill_rows<MIX>, dim3(p.tiles), block, 0, st, r);
+  // few tiles: more waves to a tile (one of 60,000 classes 26 us with 4, 12 with 16; 313 of 5003 40 and 38; 1563 of
+  // 1030 9 and 17)
+  if (p.tiles <= DISTILL_SLOTS) hipLaunchKernelGGL((k_distill_rows<MIX, 16>), dim3(p.tiles), dim3(64 * 16), 0, st, r);
+  else hipLaunchKernelGGL((k_distill_rows<MIX, 4>), dim3(p.tiles), dim3(64 * 4), 0, st, r);
   if constexpr (MODE != 0) {
     const size_t lds = 4 * (2 * r.a.k * 64 + WIDE_WAVES * distill_tile_floats(16));
     hipLaunchKernelGGL((k_distill_range<MODE, MIX>), blocks(p.ranges * p.slots), block, lds, st, r, p.ranges * p.slots);

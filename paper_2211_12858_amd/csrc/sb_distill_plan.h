@@ -50,7 +50,9 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
 }
 
 // Wider rows: the statistics of column ranges first, then the outputs range by range.
-constexpr int DISTILL_RANGE = 512;     // columns per block at most, a quarter per wave
+// columns per block at most, a quarter per wave (20,001 x 5003 with 64 places: the outputs 294 us, 309 with 512 and 312
+// with 256, which bring the lists more often)
+constexpr int DISTILL_RANGE = 640;
 constexpr int DISTILL_SLOTS = 512;     // row tiles in flight, and norm partials per column at most
 constexpr int DISTILL_BLOCKS = 1024;   // fewer (tile, range) pairs than that take narrower ranges
 

@@ -432,9 +432,11 @@ __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
     float x[2][CH];
     load(x[0], j0);
     for (int j = j0; j < j1; j += 2 * CH) {
+      wait_loads();
       if (j + CH < j1) load(x[1], j + CH);
       step(x[0], j);
       if (j + CH < j1) {
+        wait_loads();
         if (j + 2 * CH < j1) load(x[0], j + 2 * CH);
         step(x[1], j + CH);
       }
@@ -729,7 +731,7 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     }
     // the row is here; told so, the compiler waits for nothing among the sums below, where
     // the next one's scores are on their way
-    __builtin_amdgcn_s_waitcnt(0x0f70);  // vmcnt(0)
+    wait_loads();
     const int64_t next_row = row + stride;
     const int y_now = y;
     const float ay = y >= 0 && y < a.d ? to_f32(ay_raw) : 0.0f;
