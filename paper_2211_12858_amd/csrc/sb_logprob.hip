@@ -319,7 +319,7 @@ struct LaneRow {
     m = mn;
     if (a.rank) {
 #pragma unroll
-      for (int i = 0; i < CH; ++i) before += x[i] > ay || (x[i] == ay && j0 + i < y);
+      for (int i = 0; i < CH; ++i) before += (x[i] > ay) | ((x[i] == ay) & (j0 + i < y));
     }
     if (KM > 0 && !QUEUED && first) {
       start(x, j0, a.k);
