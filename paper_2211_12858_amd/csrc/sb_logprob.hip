@@ -73,7 +73,28 @@ __device__ inline void decode(u32x4& raw, Score<T> (&x)[16 / sizeof(T)]) {
     for (int u = 0; u < (int)(16 / sizeof(T)); ++u) x[u] = to_f32(e[u]);
   }
 }
-// Their maximum (of numbers).
+// The maxima (of numbers) of their first and second halves.  As it stands: the compiler
+// would round bf16 maxima to bf16 again.
+__device__ inline void halves_max(const u32x4& raw, const _Float16 (&)[8], float (&m)[2]) {
+  uint32_t p[2];
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(p[0]) : "v"(raw.x), "v"(raw.y));
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(p[1]) : "v"(raw.z), "v"(raw.w));
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    _Float16 h[2];
+    __builtin_memcpy(h, &p[i], 4);
+    const float x = (float)h[0], y = (float)h[1];
+    asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m[i]) : "v"(x), "v"(y));
+  }
+}
+template <int N>
+__device__ inline void halves_max(const u32x4&, const float (&x)[N], float (&m)[2]) {
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int u = i * N / 2; u < (i + 1) * N / 2; u += 2)
+      asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m[i]) : "v"(x[u]), "v"(x[u + 1]));
+}
 __device__ inline float max_of(const u32x4& raw, const _Float16 (&)[8]) {
   uint32_t a, b;
   asm("v_pk_max_f16 %0, %1, %2" : "=v"(a) : "v"(raw.x), "v"(raw.y));
@@ -87,7 +108,7 @@ template <int N>
 __device__ inline float max_of(const u32x4&, const float (&x)[N]) {
   float m = x[N - 1];
 #pragma unroll
-  for (int u = 0; u + 1 < N; u += 2) {  // as it stands: the compiler would round bf16 maxima to bf16 again
+  for (int u = 0; u + 1 < N; u += 2) {
     if (u + 2 < N) asm("v_max3_f32 %0, %0, %1, %2" : "+v"(m) : "v"(x[u]), "v"(x[u + 1]));
     else asm("v_max_f32 %0, %0, %1" : "+v"(m) : "v"(x[u]));
   }
@@ -581,10 +602,6 @@ __global__ void __launch_bounds__(256) k_join(LogProbArgs a) {
 // NT threads per row, E elements each; ROWS rows per block.
 // Places for collected scores, and half as many for 16-byte pieces of the row.
 constexpr int CAND_WAVE = 256, CAND_BLOCK = 1024;
-// Longest lists bounded by 64 maxima; longer ones by 128 (64 of the smallest maxima
-// would let several hundred scores through).
-constexpr int BOUND_ONE = 32;
-
 // Order-preserving bits of a score (both zeros alike), and back.
 __device__ inline uint32_t score_key(float v) {
   const uint32_t b = __float_as_uint(v + 0.0f);
@@ -679,6 +696,10 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
   };
   // what is left past the last whole 16 bytes is one score per thread
   const int whole = a.d & ~(VEC - 1);
+  // The maxima that bound a list: 64, or one for every 16 bytes of a shorter row; both
+  // halves' where the list is longer than half of them (the smallest of the maxima would
+  // let too many scores through, and fewer than k would bound nothing).
+  const int keys = whole / VEC < 64 ? whole / VEC : 64;
   auto row_at = [&](int64_t r) { return static_cast<const T*>(a.F) + r * a.ld; };
   auto load_vec = [&](const T* F, int q) {
     const uint32_t none = excluded(T());
@@ -718,7 +739,7 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     // the compiler sees the thread anew in every row: the places of its scores, a
     // register each, would otherwise be held across the rows
     asm volatile("" : "+v"(tid));
-    // the maxima of the even vectors and of the odd ones
+    // the maxima of the first halves of the 16 bytes and of the second ones
     const float tail = whole + tid < a.d ? to_f32(tail_raw) : -INFINITY;
     float lm[2] = {tail, -INFINITY};
 #pragma unroll
@@ -726,8 +747,8 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
       if (q * NT * VEC >= whole) continue;
       Score<T> x[VEC];
       decode<T>(raw[q], x);
-      lm[q & 1] = fmaxf(lm[q & 1], max_of(raw[q], x));
-      asm volatile("" : "+v"(lm[q & 1]));
+      halves_max(raw[q], x, lm);
+      asm volatile("" : "+v"(lm[0]), "+v"(lm[1]));
     }
     // the row is here; told so, the compiler waits for nothing among the sums below, where
     // the next one's scores are on their way
@@ -752,7 +773,7 @@ __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT
     m = wave_max(m);
     float b = INFINITY;  // candidates are the scores from here on
     if (a.k > 0) {
-      const uint32_t kb = a.k > BOUND_ONE ? key_bound<true>(score_key(lm[0]), score_key(lm[1]), a.k)
+      const uint32_t kb = 2 * a.k > keys ? key_bound<true>(score_key(lm[0]), score_key(lm[1]), a.k)
                                           : key_bound<false>(score_key(fmaxf(lm[0], lm[1])), 0, a.k);
       // -inf is no candidate; the lowest score above it is -FLT_MAX
       b = kb > KEY_EXCLUDED ? key_score(kb) : -FLT_MAX;
