@@ -972,10 +972,12 @@ struct RowsByLane {
 template <typename T>
 void launch_rows(LogProbArgs a, hipStream_t st) {
   // A lane per row where there are rows for the lanes of the card: its time is that of
-  // d columns until there are some 100,000 rows, a wave's that of the rows.  (us at
-  // fp32, 5 alternatives, by lane and by wave: 10,000 x 40 12.5 and 11.6, 50,000 x 200 33
-  // and 49, 50,000 x 800 84 and 64, 200,000 x 800 166 and 235; fp16 with 16: 298 and 273.)
-  if (a.n >= (int64_t)160 * a.d && a.d <= 640) {
+  // d columns until there are some 100,000 rows, a wave's that of the rows.  16-bit
+  // scores are half the bytes for a wave and the same work for a lane.  (us by lane and
+  // by wave: fp32, 5 alternatives, 20,000 x 125 20 and 19, 50,000 x 312 40 and 46,
+  // 200,000 x 640 134 and 189; fp16, 16 alternatives, 20,000 x 125 29 and 24, 200,000 x
+  // 640 238 and 206, 200,000 x 300 137 and 180, 500,000 x 600 399 and 504.)
+  if (a.n >= (int64_t)(sizeof(T) == 2 ? 480 : 160) * a.d && a.d <= 640) {
     by_list<RowsByLane<T>::template With>(a.k, a, dim3((a.tiles + 3) / 4), st);
     return;
   }
