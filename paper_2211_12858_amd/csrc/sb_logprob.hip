@@ -7,17 +7,21 @@
 //   entropy = log s - ln 2 t / s
 // (log s >= 0 >= t, so the entropy has no cancellation).
 //
-// k_rows_by_lane: one lane per row, the columns in order, 16 at a time: a running
-//   maximum, the two sums rescaled when it grows, and the best classes so far as a
-//   sorted list in registers; a score enters it if it is above the last one (equal
-//   scores stay behind the earlier class).  Column-major scores are read as runs of
-//   a column; row-major ones go through an LDS tile of 128 bytes of 64 rows.  Where
-//   there are few rows the columns are split over waves, and k_join joins the
-//   partial statistics and lists, one wave per row.
+// k_cols_by_lane, k_rows_by_lane: one lane per row, the columns in order, 16 at a
+//   time: a running maximum, the two sums rescaled when it grows, and the best classes
+//   so far as a sorted list in registers; a score enters it if it is above the last one
+//   (equal scores stay behind the earlier class).  Column-major scores are read as runs
+//   of a column; row-major ones go through an LDS tile of 128 bytes of 64 rows.  Where
+//   there are few rows the columns are split over waves, and k_join joins the partial
+//   statistics and lists.
 // k_row_in_block (row-major): a row in the registers of a wave or of a block.  The
-//   k-th largest of 64 lane maxima bounds the k-th largest score from below; the
+//   k-th largest of the threads' maxima bounds the k-th largest score from below; the
 //   scores not under it, seldom many more than k, are collected in LDS and ranked
 //   there by counting.
+//
+// Every score is read from memory once.  Its exponential takes 4 issue slots and the
+// rest 7 to 10, about what its bytes take; lists and joins come on top, so that vector
+// instructions bound all of these.
 #include <hip/hip_bf16.h>
 #include <hip/hip_fp16.h>
 
@@ -316,8 +320,8 @@ struct LaneRow {
   // j0 + i once more, for i that differs from lane to lane.  Long lists take the scores
   // above their last place through a queue in LDS (a place every 64 doubles), 16 at a
   // time or with the row's end; short ones take them one at a time, all lanes until the
-  // slowest is through.  (300,007 x 1000 with 32 alternatives 309 us, 399 one at a time;
-  // 2M x 100 with 10 alternatives 346 us, 291 one at a time.)
+  // slowest is through.  (When this was chosen: 300,007 x 1000 with 32 alternatives 309 us
+  // by queue and 399 one at a time, 2M x 100 with 10 alternatives 346 and 291.)
   template <typename Again>
   __device__ __forceinline__ void step(const LogProbArgs& a, const float (&x)[CH], int j0, int y, float ay, bool end,
                                        bool first, double* queue, Again again) {
@@ -399,6 +403,11 @@ struct ColsShared {
   double queue[LaneRow<KM>::QUEUED ? 64 * QUEUE : 1];
 };
 
+// Column-major: lanes on consecutive rows, so that every load is a run of a column; the
+// next step's 16 loads are on their way during a step.  No lane needs another one.
+// Bound by vector instructions: they fill the issue slots at 2M x 100 with 10 alternatives (240 us, 4.2 TB/s of the needed bytes)
+// and 0.72 of them at 300,007 x 1000 with 32 (300 us, 4.3 TB/s), where lists leave
+// registers for three waves per SIMD.
 template <int KM>
 __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
   __shared__ __align__(16) ColsShared<KM> sh[4];
@@ -467,6 +476,7 @@ __global__ void __launch_bounds__(256) k_cols_by_lane(LogProbArgs a) {
 }
 
 // Row-major: 128 bytes of each of 64 rows at a time, eight lanes a row, through LDS.
+// (200,000 x 640 fp32 with 5 alternatives 134 us, 3.9 TB/s; 1M x 30 64 us.)
 template <typename T, int KM>
 __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
   constexpr int VEC = 16 / sizeof(T), COLS = 8 * VEC;
@@ -533,7 +543,8 @@ __global__ void __launch_bounds__(256) k_rows_by_lane(LogProbArgs a) {
   if (lane <= left) finish_lane<KM>(a, r, row, 0, y, ay);
 }
 
-// The splits' statistics and lists of a row joined by G lanes, lane per split.  Each
+// The splits' statistics and lists of a row joined by G lanes, lane per split (20,000 x
+// 1000 with 10 alternatives: 47 us with the splits' own pass, 93 with a wave per row).  Each
 // lane has its list's next place and the one after it in hand; the best of the G next
 // places is the row's next alternative.
 template <int CTRL>
@@ -683,8 +694,13 @@ __device__ inline void ranked(const RowShared<NT>& sh, int found, int k, int tid
   }
 }
 
-// Rows of NT threads, E scores each, one after the other: a row's scores are brought
-// while the alternatives of the row before are ranked.
+// Rows of NT threads, E scores each, one after the other.  As many rows as fit are in
+// registers at once, so a row is read once, and its 16 bytes make way for those of the
+// next row as soon as they are summed: loads and arithmetic overlap in every wave
+// (4096 x 65,000 bf16 with 20 alternatives 177 us with the loads after the sums).
+// Bound by vector instructions: 0.84 of the issue slots at that shape (138 us, 3.9 TB/s),
+// 0.86 at 200,001 x 1000 fp16 with 16 alternatives (208 us), where a row's 500
+// instructions are more for its list and its joins than for its scores.
 template <typename T, int NT, int E>
 __device__ __forceinline__ void rows_in_block(const LogProbArgs& a, RowShared<NT>& sh, int64_t row, int64_t stride) {
   constexpr int VEC = 16 / sizeof(T), NV = E / VEC, W = NT / 64, CAP = RowShared<NT>::CAP;
