@@ -26,8 +26,8 @@
 //   300,007 x 1000 with hessians and 32 places 1280 us, 2.9 TB/s: one block of 16
 //   waves per CU holds 32 rows, and columns of an odd number of rows start anywhere in
 //   a cache line (300,032 rows 950 us); vector instructions take 0.31 of the issue slots.
-//   The loss alone: 1,000,003 x 100 with 10 places 133 us, 3.6 TB/s: waiting for a
-//   tile's maxima and the listed scores (0.34 of the issue slots).
+//   The loss alone: 1,000,003 x 100 with 10 places 107 us, 4.5 TB/s: the bytes (134 us
+//   with the listed scores read from memory).
 // k_loss_by_lane: the loss alone of many rows with short lists, a wave per tile.
 // k_distill_stats, k_distill_rows, k_distill_range (wider rows): maxima and sums of
 //   column ranges, then every row's statistics, targets and loss, then the outputs range
@@ -58,6 +58,7 @@ struct RowArgs {
   double* npart;    // [d][parts] or NULL
   int parts;
   int waves, groups, tiles;
+  int tile_bytes;  // of LDS per row tile
   float* stats;  // [ranges][3][n]: k_distill_stats; later [ranges][n]: k_distill_range
   float* row;    // [ROW_VALUES + k][n]: k_distill_rows
   int ranges, cols, slots;
@@ -246,17 +247,19 @@ struct WaveTile {
   }
 };
 
-// The loss alone: each wave reads the scores of the classes that its share of the
-// places lists, which its block's columns have just brought, so nothing goes through
-// the tile and the next tile's scores are on their way from the sums on.
+// The loss alone: the tile's scores go into LDS, a run of rows per column, where the
+// waves find those of the classes that their share of the places lists (in memory each
+// is a cache line of its own); the next tile's are on their way from the sums on.
 template <int ROWS, int C, bool MIX, bool FULLC, typename OFF>
 __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, int rg, int bx, int grid) {
   constexpr int PARTS = 64 / ROWS;
   const DistillArgs& a = r.a;
   const int W = r.waves, K = a.k;
   const int lane = threadIdx.x & 63, hb = lane / ROWS;
-  const WaveTile<ROWS, C, FULLC, OFF> wt{a, reinterpret_cast<float*>(lds) + 2 * K * ROWS, W, w, lane, lane & (ROWS - 1), hb,
-                                    r.groups, rg, w * C * PARTS, a.d - 1 - w * C * PARTS};
+  float* scores = reinterpret_cast<float*>(lds);  // [d][ROWS]
+  const int rl = lane & (ROWS - 1);
+  const WaveTile<ROWS, C, FULLC, OFF> wt{a, scores + a.d * ROWS, W, w, lane, rl, hb, r.groups, rg, w * C * PARTS,
+                                         a.d - 1 - w * C * PARTS};
   const int s0 = w * PARTS + hb, step = W * PARTS;
   int64_t base;
   uint32_t loc;
@@ -273,20 +276,20 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
   int next_y = a.w > 0.0 ? a.labels[base + loc] : -1;
   for (int t = bx; t < r.tiles; t += grid) {
     const int64_t row = base + loc;
-    auto score = [&](int id) { return id >= 0 ? a.F[(int64_t)id * a.ld_f + row] : 0.0f; };
+    auto score = [&](int id) { return scores[(id >= 0 ? id : 0) * ROWS + rl]; };
     Place now[AHEAD];
-    float xc[AHEAD];
     float vm = -INFINITY;
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u) {
       now[u] = usable(a, ahead[u]);
-      xc[u] = score(now[u].id);
       vm = fmaxf(vm, now[u].v);
     }
+#pragma unroll
+    for (int i = 0; i < C; ++i)
+      if (FULLC || hb * C + i <= wt.last) scores[(wt.j0 + hb * C + i) * ROWS + rl] = x[i];
 #pragma unroll 4
     for (int sl = s0 + AHEAD * step; sl < K; sl += step) vm = fmaxf(vm, usable(a, load_place(a, sl, row)).v);
     const int y = next_y < a.d ? next_y : -1;
-    const float xy = w == 0 ? score(y) : 0.0f;
     float m = x[0];
 #pragma unroll
     for (int i = 1; i < C; ++i) m = fmaxf(m, x[i]);
@@ -298,6 +301,8 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
       lds_barrier();
       m = wt.max_of(0);
       vm = wt.max_of(1);
+    } else {
+      wave_sync();
     }
     m = fmaxf(m, -FLT_MAX);  // a row of -inf has z = -inf, not differences of infinities
     float s1 = 0.0f, sT = 0.0f;
@@ -330,11 +335,12 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
     };
 #pragma unroll
     for (int u = 0; u < AHEAD; ++u)
-      if (s0 + u * step < K) add(now[u], xc[u]);
+      if (s0 + u * step < K) add(now[u], score(now[u].id));
     for (int sl = s0 + AHEAD * step; sl < K; sl += step) {
       const Place p = usable(a, load_place(a, sl, row));
       add(p, score(p.id));
     }
+    const float xy = w == 0 ? score(y) : 0.0f;
     zs = wt.part_sum(zs);
     us = wt.part_sum(us);
     ds = wt.part_sum(ds);
@@ -362,6 +368,7 @@ __device__ __forceinline__ void loss_wave(const RowArgs& r, char* lds, int w, in
       const float dot = product(te.wt, ds) + (y >= 0 ? product(A, xy - m) : 0.0f);
       if (hb == 0) a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT)) - dot;
     }
+    if (W == 1) wave_sync();  // the scores are read before the next tile's
     base = nbase;
     loc = nloc;
   }
@@ -608,7 +615,8 @@ __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs
   if (bx >= grid) return;
   const int wv = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int rg = wv / r.waves, w = wv - rg * r.waves;
-  const int bytes = 4 * (2 * r.a.k * ROWS + DISTILL_RED * r.waves * 64 + r.waves * distill_tile_floats(C));
+  const int bytes =
+      MODE == 0 ? r.tile_bytes : 4 * (2 * r.a.k * ROWS + DISTILL_RED * r.waves * 64 + r.waves * distill_tile_floats(C));
   char* lds = smem + rg * bytes;
   const bool full = (w + 1) * C * (64 / ROWS) <= r.a.d;  // all columns of the wave exist
   if constexpr (MODE == 0) {
@@ -1032,10 +1040,10 @@ __global__ void __launch_bounds__(256) k_distill_hrow(const float* sums, int ran
 }
 
 // The loss alone, a wave per tile: where there are tiles for the waves of the card, and
-// few listed scores, which by then are read from memory once more, a cache line each
-// (100,000 x 1000: 10 places 87 us, 143 by blocks; 300,007 rows: x 400, 10 places 135 and
-// 142, x 1000, 32 places 379 and 380; 1M x 100, 10 places 157 and 131).
-bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 30 * a.k; }
+// few listed scores, which by then are read from memory once more, a cache line each (us
+// by lane and by blocks: 100,000 x 1000 with 10 places 85 and 118, x 400 42 and 54;
+// 300,007 x 1000 with 32 377 and 387; 1M x 200 with 5 198 and 188, x 100 with 10 157 and 107).
+bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 40 * a.k; }
 
 template <int ROWS, int C, int MODE, typename OFF>
 void launch_regs(const RowArgs& r, const DistillPlan& p, bool mix, hipStream_t st) {
@@ -1106,7 +1114,8 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
     if (mix) hipLaunchKernelGGL(k_loss_by_lane<true>, blocks, dim3(256), 0, st, r);
     else hipLaunchKernelGGL(k_loss_by_lane<false>, blocks, dim3(256), 0, st, r);
   } else if (a.d <= DISTILL_REGS_MAX_D) {
-    const DistillPlan p = distill_plan(a.n, a.d, a.k);
+    const DistillPlan p = distill_plan(a.n, a.d, a.k, mode == 0);
+    r.tile_bytes = p.lds / p.groups;
     r.waves = p.waves;
     r.groups = p.groups;
     r.tiles = p.tiles;

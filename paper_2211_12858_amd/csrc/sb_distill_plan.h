@@ -26,7 +26,13 @@ struct DistillPlan {
 
 constexpr int distill_tile_floats(int c) { return 64 * ((c < 16 ? c : 16) + 4); }
 
-constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
+// Floats of a row tile in LDS besides what its waves exchange: the loss keeps the tile's
+// scores, the gradients the places and a tile of 16 columns for every wave.
+constexpr int distill_lds_floats(const DistillPlan& p, int32_t d, int32_t k, bool loss) {
+  return loss ? d * p.rows : 2 * k * p.rows + p.waves * distill_tile_floats(p.c);
+}
+
+constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k, bool loss = false) {
   DistillPlan p{};
   p.rows = d <= DISTILL_ONE_PART_D ? 64 : 32;
   p.c = d <= 8 ? 8 : d <= 64 ? 16 : 32;
@@ -34,7 +40,7 @@ constexpr DistillPlan distill_plan(int64_t n, int32_t d, int32_t k) {
   p.waves = (d + cols - 1) / cols;
   // narrow rows: blocks of four waves, unless there are few tiles for the CUs
   p.groups = p.waves > 2 || n < 64 * 1024 ? 1 : 4 / p.waves;
-  p.lds = p.groups * 4 * (2 * k * p.rows + DISTILL_RED * p.waves * 64 + p.waves * distill_tile_floats(p.c));
+  p.lds = p.groups * 4 * (distill_lds_floats(p, d, k, loss) + DISTILL_RED * p.waves * 64);
   const int64_t rows = (int64_t)p.rows * p.groups;
   p.tiles = (int)((n + rows - 1) / rows);
   // blocks that fit on 256 CUs at once by waves and LDS, all with the same number of tiles but the last ones
