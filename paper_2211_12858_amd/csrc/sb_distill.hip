@@ -31,8 +31,10 @@
 // k_loss_by_lane: the loss alone of many rows with short lists, a wave per tile.
 // k_distill_stats, k_distill_rows, k_distill_range (wider rows): maxima and sums of
 //   column ranges, then every row's statistics, targets and loss, then the outputs range
-//   by range.  F is read twice; 20,001 x 5003 with hessians and 64 places 131, 37 and
-//   295 us, the last 4.1 TB/s.
+//   by range, with what each range's targets take off the loss (k_distill_join adds
+//   them up; listed scores read from memory in k_distill_rows took 86 us more).  F is
+//   read twice; 20,001 x 5003 with hessians and 64 places 111, 12 and 261 us, the last
+//   4.6 TB/s.
 //
 // exp(z / T) is 2^(z * log2(e) / T) by the hardware's exponential, which returns 0
 // below 2^-126: probabilities under 2^-126 of the row's largest are 0.
@@ -59,7 +61,7 @@ struct RowArgs {
   int parts;
   int waves, groups, tiles;
   int tile_bytes;  // of LDS per row tile
-  float* stats;  // [ranges][3][n]: k_distill_stats; later [ranges][n]: k_distill_range
+  float* stats;  // [ranges][3][n]: k_distill_stats; later [ranges][2][n]: k_distill_range
   float* row;    // [ROW_VALUES + k][n]: k_distill_rows
   int ranges, cols, slots;
 };
@@ -802,7 +804,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_stats(RowArgs r, in
 }
 
 // What the rows' outputs need besides their scores: the joined statistics, the
-// targets of the listed places and the loss.  64 rows per block, ranges and places
+// targets of the listed places and the loss (with gradients, its part without scores).  64 rows per block, ranges and places
 // shared out among its waves.  In the workspace of n floats each:
 //   row[0] max, row[1] coefficient of 2^(z c2) in g, row[2] of 2^(z log2 e),
 //   row[3] 1 / sT, row[4] 1 / s1, row[5] Q, then the targets of the K places.
@@ -871,9 +873,12 @@ __global__ void __launch_bounds__(64 * WAVES) k_distill_rows(RowArgs r) {
     const Place p = usable(a, load_place(a, s, row));
     const float t = te.wt * place_exp(r, p.v, vm, unused);
     if (a.G) targets[s * a.n] = t;
-    if (a.loss && p.id >= 0) dot += product(t, a.F[(int64_t)p.id * a.ld_f + row] - m);
+    // with gradients the ranges, which have the scores at hand, form the products
+    if (!a.G && p.id >= 0) dot += product(t, a.F[(int64_t)p.id * a.ld_f + row] - m);
   }
-  if (a.loss) {
+  if (a.loss && a.G) {
+    if (w == 0) a.loss[row] = A * log_of(s1) + r.bt * (te.ent + te.Q * log_of(sT));
+  } else if (a.loss) {
     if (w == 0 && y >= 0) dot += product(A, a.F[(int64_t)y * a.ld_f + row] - m);
     red[0][w][lane] = dot;  // the maxima are read before the barrier above
     __syncthreads();
@@ -895,7 +900,7 @@ __global__ void __launch_bounds__(64 * WAVES) k_distill_rows(RowArgs r) {
 template <int MODE, bool MIX>
 __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, int units) {
   extern __shared__ __align__(16) char smem[];
-  __shared__ float red[WIDE_WAVES][64];
+  __shared__ float red[2][WIDE_WAVES][64];
   const DistillArgs& a = r.a;
   const int K = a.k;
   const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -934,7 +939,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, in
     const float hQ = r.b * Q * r.inv_t;
     const float hT = MIX ? hQ : A + hQ, h1 = A;
     __syncthreads();
-    float hsum = 0.0f;
+    float hsum = 0.0f, dot = 0.0f;
     // the places of the wave's columns, a bit each; every group takes its own out
     uint64_t mine = 0;
 #pragma unroll 8
@@ -981,6 +986,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, in
             e1 = exp2_hw(z * LOG2E);
             gr = fmaf(k1, e1, gr);
           }
+          dot += product(tv[u], z);  // columns past the last repeat it without a target
           // rows past the end store row n - 1's own values once more
           if (live) Gc[loc] = gr;
           Gc += a.ld_g;
@@ -1018,25 +1024,35 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, in
       if (last >= 15) group(std::true_type(), c0, last);
       else group(std::false_type(), c0, last);
     }
-    if (MODE == 2 && a.h_row) {
-      red[w][lane] = hsum;
+    if (a.loss || (MODE == 2 && a.h_row)) {
+      red[0][w][lane] = dot;
+      red[1][w][lane] = hsum;
       __syncthreads();
-      if (w == 0 && ok) {
-        for (int u = 1; u < WIDE_WAVES; ++u) hsum += red[u][lane];
-        r.stats[(int64_t)range * a.n + row] = hsum;  // the ranges' statistics are read by now
+      if (w == 0 && ok) {  // the ranges' statistics are read by now
+        for (int u = 1; u < WIDE_WAVES; ++u) {
+          dot += red[0][u][lane];
+          hsum += red[1][u][lane];
+        }
+        r.stats[(int64_t)range * 2 * a.n + row] = dot;
+        r.stats[((int64_t)range * 2 + 1) * a.n + row] = hsum;
       }
     }
     __syncthreads();  // the places and exchanged values are read before the next tile's
   }
 }
 
-// Row means of the hessians from the ranges' sums.
-__global__ void __launch_bounds__(256) k_distill_hrow(const float* sums, int ranges, int64_t n, int d, float* h_row) {
+// The ranges' sums of a row: what its targets take off the loss, and its hessians' mean.
+__global__ void __launch_bounds__(256) k_distill_join(const float* sums, int ranges, int64_t n, int d, float* loss,
+                                                      float* h_row) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
-  float s = 0.0f;
-  for (int q = 0; q < ranges; ++q) s += sums[(int64_t)q * n + i];
-  h_row[i] = s * (1.0f / (float)d);
+  float dot = 0.0f, h = 0.0f;
+  for (int q = 0; q < ranges; ++q) {
+    dot += sums[(int64_t)q * 2 * n + i];
+    h += sums[((int64_t)q * 2 + 1) * n + i];
+  }
+  if (loss) loss[i] -= dot;
+  if (h_row) h_row[i] = h * (1.0f / (float)d);
 }
 
 // The loss alone, a wave per tile: where there are tiles for the waves of the card, and
@@ -1068,16 +1084,16 @@ void launch_wide(const RowArgs& r, const DistillWidePlan& p, hipStream_t st) {
   const dim3 block(64 * WIDE_WAVES);
   auto blocks = [](int units) { return dim3((units + 7) / 8 * 8); };
   hipLaunchKernelGGL(k_distill_stats<MIX>, blocks(p.ranges * p.tiles), block, 0, st, r, p.ranges * p.tiles);
-  // few tiles: more waves to a tile (one of 60,000 classes 26 us with 4, 12 with 16; 313 of 5003 40 and 38; 1563 of
+  // few tiles: more waves to a tile (one of 60,000 classes 26 us with 4, 12 with 16; 313 of 5003 12 with 16; 1563 of
   // 1030 9 and 17)
   if (p.tiles <= DISTILL_SLOTS) hipLaunchKernelGGL((k_distill_rows<MIX, 16>), dim3(p.tiles), dim3(64 * 16), 0, st, r);
   else hipLaunchKernelGGL((k_distill_rows<MIX, 4>), dim3(p.tiles), dim3(64 * 4), 0, st, r);
   if constexpr (MODE != 0) {
     const size_t lds = 4 * (2 * r.a.k * 64 + WIDE_WAVES * distill_tile_floats(16));
     hipLaunchKernelGGL((k_distill_range<MODE, MIX>), blocks(p.ranges * p.slots), block, lds, st, r, p.ranges * p.slots);
-    if (r.a.h_row)
-      hipLaunchKernelGGL(k_distill_hrow, dim3((unsigned)((r.a.n + 255) / 256)), dim3(256), 0, st, r.stats, p.ranges, r.a.n,
-                         r.a.d, r.a.h_row);
+    if (r.a.loss || r.a.h_row)
+      hipLaunchKernelGGL(k_distill_join, dim3((unsigned)((r.a.n + 255) / 256)), dim3(256), 0, st, r.stats, p.ranges, r.a.n,
+                         r.a.d, r.a.loss, r.a.h_row);
   }
 }
 
