@@ -25,7 +25,8 @@
 //   2M x 100 with labels and 10 places 403 us, 4.4 TB/s of 4.7 in a copy: the bytes.
 //   300,007 x 1000 with hessians and 32 places 1280 us, 2.9 TB/s: one block of 16
 //   waves per CU holds 32 rows, and columns of an odd number of rows start anywhere in
-//   a cache line (300,032 rows 950 us); vector instructions take 0.31 of the issue slots.
+//   a cache line, so that half as many requests again go to the L2 (300,032 rows 950 us);
+//   vector instructions take a third of the issue slots.
 //   The loss alone: 1,000,003 x 100 with 10 places 107 us, 4.5 TB/s: the bytes (134 us
 //   with the listed scores read from memory).
 // k_loss_by_lane: the loss alone of many rows with short lists, a wave per tile.
