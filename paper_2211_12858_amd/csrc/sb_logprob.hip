@@ -179,7 +179,7 @@ __device__ inline void store_row(const LogProbArgs& a, int64_t row, const RowSta
   if (a.lse) a.lse[row] = none ? -INFINITY : fmaf(r.m, a.c, ls);
   if (a.entropy) a.entropy[row] = none || h < 0.0f ? 0.0f : h;
   if (a.logp) a.logp[row] = !has ? 0.0f : none ? -INFINITY : (ay - r.m) * a.c - ls;
-  if (a.rank) a.rank[row] = has ? before : -1;
+  if (a.rank) a.rank[row] = has ? min(before, a.d - 1) : -1;  // a NaN compares with no score
 }
 __device__ inline void store_top(const LogProbArgs& a, int64_t row, int place, float v, int id, const RowStats& r,
                                  float ls) {

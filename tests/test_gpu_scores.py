@@ -290,6 +290,23 @@ def test_nan_and_inf_stay_in_their_row(order, dtype, d):
     check(F, got, 1.0, y, 2, np.setdiff1d(np.arange(70), [3, 66]))
 
 
+@pytest.mark.parametrize("order,dtype", CASES)
+@pytest.mark.parametrize("d", [3, 100, 1001, 9001])
+def test_ranks_and_classes_of_nan_rows_are_in_range(order, dtype, d):
+    rng = np.random.default_rng(d)
+    n, k = 70, 20
+    F = rounded(rng.normal(size=(n, d)), dtype)
+    F[::2, rng.integers(0, d, 5)] = np.nan
+    F[1::4] = np.nan
+    F[3::4, d - 1] = np.inf
+    y = np.full(n, d - 1, dtype=np.int32)
+    F[0::8, d - 1] = np.nan  # the given class itself
+    got = run(F, order, dtype, 1.0, y, k)
+    assert got["rank"].min() >= 0 and got["rank"].max() < d
+    assert got["top_id"].min() >= -1 and got["top_id"].max() < d
+    assert np.isnan(got["lse"]).all() and np.isnan(got["logp"]).all() and np.isnan(got["entropy"]).all()
+
+
 @pytest.mark.parametrize("order", ["col", "row"])
 def test_outputs_are_optional(order):
     rng = np.random.default_rng(4)
