@@ -542,7 +542,10 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
  *   SB_TEACHER_LOG_PROBS  q_t = exp(z_t);
  *   loss = w (-log p1[label]) + (1 - w) T^2 sum_t q_t (log q_t - log pT[c_t]),
  * w = hard_weight.  Places whose class is outside [0, d) are unused whatever
- * their value; a value of -inf has q_t = 0; a class may be listed twice.  Rows
+ * their value; a value of -inf has q_t = 0; a class may be listed twice.  The
+ * exponentials under q_t (of z_t / T less the list's largest, or of z_t) are 0
+ * below 2^-126, wherever in the list they stand.  A place with q_t > 0 is a
+ * target; where (1 - w) T q_t is below 2^-126 it may count as none.  Rows
  * whose label is outside [0, d) have no first term, rows with no used place
  * no second.
  *

@@ -633,8 +633,9 @@ __global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_distill_regs(RowArgs
 
 // ---------------------------------------------------------------- the loss of many rows
 // One lane per row, one wave per 64-row tile: a running maximum and sums over the
-// columns in order, then the places, eight at a time, with a running maximum of
-// their own.  No wave waits for another.
+// columns in order, then the places, eight at a time, twice: their largest value, which
+// the sums are relative to (a place is a target or not by its distance from it, wherever
+// in the list it stands), then the sums.  No wave waits for another.
 template <bool MIX>
 __global__ void __launch_bounds__(256) k_loss_by_lane(RowArgs r) {
   const DistillArgs& a = r.a;
@@ -688,28 +689,25 @@ __global__ void __launch_bounds__(256) k_loss_by_lane(RowArgs r) {
     }
   }
   if (!MIX) s1 = sT;
-  const bool logits = a.teacher == SB_TEACHER_LOGITS;
-  float vm = logits ? -FLT_MAX : 0.0f, zs = 0.0f, us = 0.0f, ds = 0.0f;
-  for (int s = 0; s < a.k; s += 8) {
-    Place p[8];
-    float xc[8];
+  float vm = -INFINITY, zs = 0.0f, us = 0.0f, ds = 0.0f;
+  auto places = [&](Place (&p)[8], int s) {
 #pragma unroll
     for (int u = 0; u < 8; ++u) p[u] = s + u < a.k ? load_place(a, s + u, row) : Place{-1, 0.0f};
 #pragma unroll
-    for (int u = 0; u < 8; ++u) {
-      p[u] = usable(a, p[u]);
-      xc[u] = p[u].id >= 0 ? F[(int64_t)p[u].id * a.ld_f + loc] : m;
-    }
-    if (logits) {
-      float vn = vm;
+    for (int u = 0; u < 8; ++u) p[u] = usable(a, p[u]);
+  };
+  Place p[8];
+  // back to front, so that a list of up to eight is read once (log probabilities need no largest value)
+  for (int s = a.teacher == SB_TEACHER_LOGITS ? (a.k - 1) & ~7 : 0; s >= 0; s -= 8) {
+    places(p, s);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) vn = fmaxf(vn, p[u].v);
-      const float du = fmaxf((vm - vn) * r.inv_t, -1000.0f), f = exp2_hw(du * LOG2E);
-      us = f * fmaf(zs, du, us);
-      zs *= f;
-      ds *= f;
-      vm = vn;
-    }
+    for (int u = 0; u < 8; ++u) vm = fmaxf(vm, p[u].v);
+  }
+  for (int s = 0; s < a.k; s += 8) {
+    if (s > 0) places(p, s);
+    float xc[8];
+#pragma unroll
+    for (int u = 0; u < 8; ++u) xc[u] = p[u].id >= 0 ? F[(int64_t)p[u].id * a.ld_f + loc] : m;
 #pragma unroll
     for (int u = 0; u < 8; ++u) {
       const float e = place_exp(r, p[u].v, vm, us);
