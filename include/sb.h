@@ -558,7 +558,10 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
  * k, t_id, t_val, ld_t  1..SB_MAX_TOP places per row: place t of row i at
  *              [t*ld_t + i], ld_t >= n (as sb_log_probs writes them).
  * loss         out: n fp32.
- * fp32 arithmetic, sums in a fixed order.
+ * Sums in a fixed order.  Up to T = 4 fp32 arithmetic: the second term is off
+ * by some roundings (2^-24) of (1 - w) T^2 Q log d.  Above, its parts are formed
+ * so that only roundings of the row's squared differences of scores and values
+ * are left of that (of T times the differences where they are beyond T / 2).
  * Workspace: sb_workspace_bytes(SB_CALL_DISTILL, n, d, k).
  */
 int32_t sb_distill_loss(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature, double hard_weight,
@@ -579,7 +582,9 @@ int32_t sb_distill_loss(const float* F, int64_t n, int32_t d, int64_t ld_f, doub
  * h_row    out (may be NULL): n fp32 row means of the hessians.
  * norm2    out (may be NULL): d fp64 values sum_i G[i, j]^2 of the stored G,
  *          added in a fixed order (deterministic).
- * Probabilities below 2^-126 of the row's largest are taken as 0.
+ * Probabilities below 2^-126 of the row's largest are taken as 0.  fp32
+ * arithmetic at every temperature: G is off by some roundings (2^-24) of the
+ * terms that it is the difference of, (1 - w) T (Q pT_j) and (1 - w) T q_t.
  * F, G and hess must not overlap.  Every other argument as sb_distill_loss.
  */
 int32_t sb_distill_gradients(const float* F, int64_t n, int32_t d, int64_t ld_f, double temperature,

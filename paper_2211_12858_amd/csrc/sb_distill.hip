@@ -37,6 +37,9 @@
 //   read twice; 20,001 x 5003 with hessians and 64 places 111, 12 and 261 us, the last
 //   4.6 TB/s.
 //
+// k_hot_loss (with k_hot_stats): the loss at T > 4, whose terms are far larger than what
+//   they add up to.
+//
 // exp(z / T) is 2^(z * log2(e) / T) by the hardware's exponential, which returns 0
 // below 2^-126: probabilities under 2^-126 of the row's largest are 0.
 #include <cfloat>
@@ -1054,6 +1057,279 @@ __global__ void __launch_bounds__(256) k_distill_join(const float* sums, int ran
   if (h_row) h_row[i] = h * (1.0f / (float)d);
 }
 
+// ---------------------------------------------------------------- the loss at high temperatures
+// The loss's terms are about T^2 log d, and what they add up to is about the squared
+// differences of scores and values: in fp32 all of it is lost at T = 1000.  Their parts of
+// order 1, 1 / T and 1 / T^2 are kept apart.  With x_j = (a_j - m) / T,
+//   exp(x) = 1 + x + phi(x),  phi(x) = x^2 / 2 + x^3 / 6 + ...,
+// 1 + x is summed in fp64 from the scores as they are, and phi, formed in fp32, carries
+// fp32 roundings of x^2: after T^2 those of the squared differences.  Where x < -1/2 the
+// exponential itself is as small as its roundings ask for.  The list's exponentials and
+// all sums and logarithms of a row are fp64.
+// Up to T = HOT the fp32 forms above lose at most four bits more than they do at T = 1.
+// Bound by vector instructions (some 25 per score, two of them in fp64) and, in lists of
+// many rows, by the listed scores, a cache line each: 1,000,003 x 100 with 10 places
+// 213 us (107 by the fp32 form), 300,007 x 1000 with 25 397 (342), 20,001 x 5003 with 64
+// 170 (111); 64 x 60,000 37 (23), of which a second launch is part.  A call for gradients
+// reads the scores once more for it.
+constexpr double HOT = 4.0;
+
+struct HotArgs {
+  RowArgs r;
+  double inv_t, bt;  // 1 / T, (1 - w) T^2
+  int waves, tiles;
+  int ranges, cols;  // k_hot_stats: column ranges; 0 if there are none
+  double* S;         // [ranges][n]
+  float2* ms;        // [ranges][n]: maximum, sum at T = 1
+};
+
+struct HotSums {
+  float m = -FLT_MAX, s1 = 0.0f;
+  double S = 0.0;  // sum exp((a - m) / T)
+};
+
+// exp(x) - 1 - x for |x| <= 1/2: the Taylor series to x^9 / 9! (the next term is 2^-25 of it)
+__device__ inline float phi(float x) {
+  float p = 1.0f / 362880.0f;
+  p = fmaf(p, x, 1.0f / 40320.0f);
+  p = fmaf(p, x, 1.0f / 5040.0f);
+  p = fmaf(p, x, 1.0f / 720.0f);
+  p = fmaf(p, x, 1.0f / 120.0f);
+  p = fmaf(p, x, 1.0f / 24.0f);
+  p = fmaf(p, x, 1.0f / 6.0f);
+  p = fmaf(p, x, 0.5f);
+  return x * x * p;
+}
+__device__ inline double exp_fine(double x) {  // x <= 0
+  const float f = (float)x;
+  return f >= -0.5f ? 1.0 + (x + (double)phi(f)) : (double)exp2_hw(f * LOG2E);
+}
+
+// h joined with the sums o of other columns of the row.
+template <bool MIX>
+__device__ inline void hot_add(HotSums& h, const HotSums& o, double inv_t) {
+  const float mn = fmaxf(h.m, o.m);
+  h.S = h.S * exp_fine(((double)h.m - mn) * inv_t) + o.S * exp_fine(((double)o.m - mn) * inv_t);
+  if (MIX) h.s1 = h.s1 * exp2_hw((h.m - mn) * LOG2E) + o.s1 * exp2_hw((o.m - mn) * LOG2E);
+  h.m = mn;
+}
+
+// The sums of columns j0 .. j1 - 1 of a lane's row; the next 16 are on their way meanwhile.
+template <bool MIX>
+__device__ inline HotSums hot_columns(const HotArgs& h, const float* F, int loc, int j0, int j1) {
+  const int64_t ld = h.r.a.ld_f;
+  const float inv_t = h.r.inv_t, c2 = h.r.c2;
+  HotSums o;
+  float x[2][16];
+  auto load = [&](float (&to)[16], int j) {
+    const float* p = F + (int64_t)j * ld;
+    if (j + 16 <= j1) {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, p += ld) to[i] = p[loc];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 16; ++i, p += ld) {
+        to[i] = -INFINITY;
+        if (j + i < j1) to[i] = p[loc];
+      }
+    }
+  };
+  auto step = [&](const float (&now)[16]) {
+    float mn = o.m;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) mn = fmaxf(mn, now[i]);
+    if (__any(mn > o.m)) {
+      o.S *= exp_fine(((double)o.m - mn) * h.inv_t);
+      if (MIX) o.s1 *= exp2_hw((o.m - mn) * LOG2E);
+      o.m = mn;
+    }
+    int near = 0;
+    double sum = 0.0;  // of the near scores
+    float f = 0.0f, s1 = 0.0f;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+      const float z = now[i] - mn, v = z * inv_t;
+      const bool is_near = v >= -0.5f;
+      const float p = phi(v), e = exp2_hw(z * c2);
+      f += is_near ? p : e;
+      sum += (double)(is_near ? now[i] : 0.0f);
+      near += is_near;
+      if (MIX) s1 += exp2_hw(z * LOG2E);
+      if (i % 4 == 3) asm volatile("" : "+v"(f), "+v"(s1), "+v"(sum));  // here and now: put off, the terms take registers
+    }
+    o.S += ((double)near + (sum - (double)near * (double)mn) * h.inv_t) + (double)f;
+    if (MIX) o.s1 += s1;
+  };
+  if (j0 < j1) load(x[0], j0);
+  for (int j = j0; j < j1; j += 32) {
+    wait_loads();
+    if (j + 16 < j1) load(x[1], j + 16);
+    step(x[0]);
+    if (j + 16 < j1) {
+      wait_loads();
+      if (j + 32 < j1) load(x[0], j + 32);
+      step(x[1]);
+    }
+  }
+  return o;
+}
+
+// What the waves of a block exchange, 64 values each.
+struct HotShared {
+  double* d;  // [4][waves][64]
+  float* f;   // [3][waves][64]
+  int waves;
+  __device__ HotShared(char* lds, int waves)
+      : d(reinterpret_cast<double*>(lds)), f(reinterpret_cast<float*>(lds + 4 * 8 * 64 * waves)), waves(waves) {}
+  __device__ double& at(int q, int w, int lane) const { return d[(q * waves + w) * 64 + lane]; }
+  __device__ float& at_f(int q, int w, int lane) const { return f[(q * waves + w) * 64 + lane]; }
+  __device__ double sum(int q, int lane) const {
+    double s = at(q, 0, lane);
+    for (int u = 1; u < waves; ++u) s += at(q, u, lane);
+    return s;
+  }
+};
+constexpr int HOT_WAVE_BYTES = 64 * (4 * 8 + 3 * 4);
+
+template <bool MIX>
+__device__ inline HotSums hot_join(const HotArgs& h, const HotShared& sh, HotSums o, int w, int lane) {
+  if (sh.waves == 1) return o;
+  sh.at(0, w, lane) = o.S;
+  sh.at_f(0, w, lane) = o.m;
+  sh.at_f(1, w, lane) = o.s1;
+  __syncthreads();
+  o = HotSums();
+  for (int u = 0; u < sh.waves; ++u)
+    hot_add<MIX>(o, HotSums{sh.at_f(0, u, lane), sh.at_f(1, u, lane), sh.at(0, u, lane)}, h.inv_t);
+  return o;
+}
+
+// A 64-row tile's sums in one column range, for k_hot_loss of few rows with many classes.
+template <bool MIX>
+__global__ void __launch_bounds__(64 * WIDE_WAVES) k_hot_stats(HotArgs h) {
+  extern __shared__ __align__(16) char smem[];
+  const HotShared sh(smem, WIDE_WAVES);
+  const DistillArgs& a = h.r.a;
+  const int range = blockIdx.x / h.tiles, tile = blockIdx.x - range * h.tiles;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t base = (int64_t)tile * 64, left = a.n - 1 - base;
+  const int loc = lane < left ? lane : (int)left;
+  const int per = h.cols / WIDE_WAVES, j0 = range * h.cols + w * per;
+  const HotSums o = hot_join<MIX>(h, sh, hot_columns<MIX>(h, a.F + base, loc, j0, j0 + per < a.d ? j0 + per : a.d), w, lane);
+  if (w != 0 || lane > left) return;
+  const int64_t at = (int64_t)range * a.n + base + lane;
+  h.S[at] = o.S;
+  h.ms[at] = make_float2(o.m, o.s1);
+}
+
+// A 64-row tile per block: its columns (or the ranges' sums) and its list places shared
+// out among the waves.
+template <bool MIX>
+__global__ void __launch_bounds__(64 * DISTILL_MAX_WAVES) k_hot_loss(HotArgs h) {
+  extern __shared__ __align__(16) char smem[];
+  const HotShared sh(smem, h.waves);
+  const DistillArgs& a = h.r.a;
+  const int lane = threadIdx.x & 63, w = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), W = h.waves;
+  const int64_t base = (int64_t)blockIdx.x * 64, left = a.n - 1 - base;  // rows past the end read row n - 1
+  const int loc = lane < left ? lane : (int)left;
+  const int64_t row = base + loc;
+  HotSums o;
+  if (h.ranges) {
+    for (int q = w; q < h.ranges; q += W) {
+      const float2 ms = h.ms[(int64_t)q * a.n + row];
+      hot_add<MIX>(o, HotSums{ms.x, ms.y, h.S[(int64_t)q * a.n + row]}, h.inv_t);
+    }
+  } else {
+    const int per = ((a.d + W - 1) / W + 15) / 16 * 16, j0 = w * per;
+    o = hot_columns<MIX>(h, a.F + base, loc, j0, j0 + per < a.d ? j0 + per : a.d);
+  }
+  const bool logits = a.teacher == SB_TEACHER_LOGITS;
+  float vm = -INFINITY;
+  if (logits) {
+#pragma unroll 4
+    for (int s = w; s < a.k; s += W) vm = fmaxf(vm, usable(a, load_place(a, s, row)).v);
+    sh.at_f(2, w, lane) = vm;
+  }
+  o = hot_join<MIX>(h, sh, o, w, lane);
+  if (logits)
+    for (int u = 0; u < W; ++u) vm = fmaxf(vm, sh.at_f(2, u, lane));
+  // e_t and its products with the value and the listed score; a place with e_t = 0 is no target
+  double zs = 0.0, us = 0.0, ds = 0.0;
+  for (int s = w; s < a.k; s += 4 * W) {
+    Place p[4];
+    float score[4];
+#pragma unroll
+    for (int u = 0; u < 4; ++u) p[u] = s + u * W < a.k ? load_place(a, s + u * W, row) : Place{-1, 0.0f};
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      p[u] = usable(a, p[u]);
+      score[u] = a.F[(int64_t)(p[u].id >= 0 ? p[u].id : 0) * a.ld_f + row];
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const double x = logits ? ((double)p[u].v - (double)vm) * h.inv_t : (double)p[u].v;
+      // a value of -inf is left out here: with no finite one its difference is no number
+      const double e = p[u].v == -INFINITY ? 0.0 : logits ? exp_fine(x) : (double)exp2_hw(p[u].v * LOG2E);
+      if (e != 0.0) {
+        zs += e;
+        us += e * x;
+        ds += e * ((double)score[u] - (double)o.m);
+      }
+    }
+  }
+  if (W > 1) {
+    sh.at(1, w, lane) = zs;
+    sh.at(2, w, lane) = us;
+    sh.at(3, w, lane) = ds;
+    __syncthreads();
+  }
+  if (w != 0) return;
+  if (W > 1) {
+    zs = sh.sum(1, lane);
+    us = sh.sum(2, lane);
+    ds = sh.sum(3, lane);
+  }
+  const double log_S = o.S > 0.0 ? log(o.S) : 0.0;
+  double loss = 0.0;
+  if (!logits) loss = h.bt * (us + zs * log_S - ds * h.inv_t);
+  else if (zs != 0.0) loss = h.bt * ((us - ds * h.inv_t) / zs + (log_S - log(zs)));
+  if (MIX) {
+    const int y = a.labels[row];
+    if (y >= 0 && y < a.d)
+      loss += a.w * ((double)log_of(o.s1) - ((double)a.F[(int64_t)y * a.ld_f + row] - (double)o.m));
+  }
+  if (lane <= left) a.loss[row] = (float)loss;
+}
+
+// Few rows with many classes: column ranges over blocks.
+DistillWidePlan hot_plan(int64_t n, int32_t d) {
+  DistillWidePlan p{};
+  const int tiles = (int)((n + 63) / 64);
+  if (d > DISTILL_REGS_MAX_D && tiles < 128) p = distill_wide_plan(n, d);
+  p.tiles = tiles;
+  return p;
+}
+int64_t hot_bytes(int64_t n, int32_t d) { return align256((int64_t)hot_plan(n, d).ranges * n * 8) * 2; }
+
+void launch_hot(const RowArgs& r, void* ws, bool mix, hipStream_t st) {
+  const DistillArgs& a = r.a;
+  const DistillWidePlan p = hot_plan(a.n, a.d);
+  // eight waves per CU where the columns allow it
+  int waves = (2048 + p.tiles - 1) / p.tiles;
+  if (waves > DISTILL_MAX_WAVES) waves = DISTILL_MAX_WAVES;
+  if (waves > (a.d + 15) / 16) waves = (a.d + 15) / 16;
+  char* at = static_cast<char*>(ws);
+  const HotArgs h{r, 1.0 / a.T, (1.0 - a.w) * a.T * a.T, waves, p.tiles, p.ranges, p.cols,
+                  reinterpret_cast<double*>(at), reinterpret_cast<float2*>(at + align256((int64_t)p.ranges * a.n * 8))};
+  auto run = [&](auto stats, auto loss) {
+    if (p.ranges)
+      hipLaunchKernelGGL(stats, dim3(p.ranges * p.tiles), dim3(64 * WIDE_WAVES), WIDE_WAVES * HOT_WAVE_BYTES, st, h);
+    hipLaunchKernelGGL(loss, dim3(p.tiles), dim3(64 * waves), waves * HOT_WAVE_BYTES, st, h);
+  };
+  if (mix) run(k_hot_stats<true>, k_hot_loss<true>);
+  else run(k_hot_stats<false>, k_hot_loss<false>);
+}
+
 // The loss alone, a wave per tile: where there are tiles for the waves of the card, and
 // few listed scores, which by then are read from memory once more, a cache line each (us
 // by lane and by blocks: 100,000 x 1000 with 10 places 85 and 118, x 400 42 and 54;
@@ -1104,15 +1380,21 @@ int64_t norm_bytes(int64_t n, int32_t d, int32_t k) {
 
 }  // namespace
 
-// Workspace: [norm partials]; past 1024 classes [rows' values and targets][statistics of the ranges] too
+// Workspace: [norm partials]; past 1024 classes [rows' values and targets][statistics of the ranges] too.
+// A hot loss takes it from the start again.
 int64_t distill_ws_bytes(int64_t n, int32_t d, int32_t k) {
   int64_t b = norm_bytes(n, d, k);
   if (d > DISTILL_REGS_MAX_D)
     b += align256((int64_t)(ROW_VALUES + k) * n * 4) + align256((int64_t)distill_wide_plan(n, d).ranges * 3 * n * 4);
-  return b;
+  const int64_t hot = hot_bytes(n, d);
+  return b > hot ? b : hot;
 }
 
-int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const char* call) {
+int32_t launch_distill(const DistillArgs& args, void* ws, hipStream_t st, const char* call) {
+  // a hot loss is formed by kernels of its own, once the others are through with the workspace
+  const bool hot = args.loss && args.T > HOT && args.w < 1.0;
+  DistillArgs a = args;
+  if (hot) a.loss = nullptr;
   const double b = (1.0 - a.w) * a.T;
   RowArgs r{};
   r.a = a;
@@ -1124,7 +1406,9 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
   r.npart = a.norm2 ? static_cast<double*>(ws) : nullptr;
   const bool mix = a.w > 0.0 && a.T != 1.0;
   const int mode = !a.G ? 0 : a.hess || a.h_row ? 2 : 1;
-  if (mode == 0 && loss_by_lane(a)) {
+  if (mode == 0 && hot) {
+    // nothing else is asked for
+  } else if (mode == 0 && loss_by_lane(a)) {
     const dim3 blocks((unsigned)((a.n + 255) / 256));
     if (mix) hipLaunchKernelGGL(k_loss_by_lane<true>, blocks, dim3(256), 0, st, r);
     else hipLaunchKernelGGL(k_loss_by_lane<false>, blocks, dim3(256), 0, st, r);
@@ -1153,6 +1437,10 @@ int32_t launch_distill(const DistillArgs& a, void* ws, hipStream_t st, const cha
     else mix ? launch_wide<2, true>(r, p, st) : launch_wide<2, false>(r, p, st);
   }
   if (a.norm2) launch_norm_final(r.npart, a.d, r.parts, a.norm2, st);
+  if (hot) {
+    r.a.loss = args.loss;
+    launch_hot(r, ws, mix, st);
+  }
   return check_launch(call);
 }
 
