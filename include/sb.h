@@ -523,6 +523,8 @@ int32_t sb_update_and_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
  *            alternatives: the places past the last one get class -1 and
  *            -inf.  This is the teacher's list of the distillation calls.
  * A row whose scores are all -inf gets lse = logp = -inf and entropy 0.
+ * Everything is aligned to its element type; outputs overlap neither F, labels
+ * nor each other.
  * Sums in fp32 of terms at the row's maximum; ranks and the order of the
  * alternatives compare the scores as given, so they are exact.
  * Workspace: sb_workspace_bytes(SB_CALL_LOG_PROBS, n, d, k).
@@ -558,6 +560,8 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
  * k, t_id, t_val, ld_t  1..SB_MAX_TOP places per row: place t of row i at
  *              [t*ld_t + i], ld_t >= n (as sb_log_probs writes them).
  * loss         out: n fp32.
+ * Everything is aligned to its element type (norm2 of the next call to 8
+ * bytes); outputs overlap neither inputs nor each other.
  * Sums in a fixed order.  Up to T = 4 fp32 arithmetic: the second term is off
  * by some roundings (2^-24) of (1 - w) T^2 Q log d.  Above, its parts are formed
  * so that only roundings of the row's squared differences of scores and values

@@ -668,6 +668,19 @@ bool overlap(const void* a, int64_t a_bytes, const void* b, int64_t b_bytes) {
   return a && b && a0 < b0 + (uintptr_t)b_bytes && b0 < a0 + (uintptr_t)a_bytes;
 }
 
+// The first of them that is not aligned (NULL is), or NULL.  What a call does not use is given as NULL.
+struct Aligned {
+  const char* name;
+  const void* at;
+  uintptr_t by;
+};
+template <size_t N>
+const char* misaligned(const Aligned (&v)[N]) {
+  for (const Aligned& x : v)
+    if (!aligned(x.at, x.by)) return x.name;
+  return nullptr;
+}
+
 bool temperature_ok(double t) { return t >= 1e-4 && t <= 1e4; }
 
 int32_t check_distill(const char* call, const DistillArgs& a) {
@@ -685,6 +698,9 @@ int32_t check_distill(const char* call, const DistillArgs& a) {
   if (a.ld_t < a.n || a.ld_t > MAX_LD) return fail(SB_E_SHAPE, c + ": ld_t must be >= n");
   if (!aligned(a.F, 4) || !aligned(a.t_id, 4) || !aligned(a.t_val, 4))
     return fail(SB_E_SHAPE, c + ": F, t_id and t_val must be 4-byte aligned");
+  if (const char* name = misaligned({{"labels", a.w > 0.0 ? a.labels : nullptr, 4}, {"loss", a.loss, 4}, {"G", a.G, 4}, {"hess", a.hess, 4},
+                                     {"h_row", a.h_row, 4}, {"norm2", a.norm2, 8}}))
+    return fail(SB_E_SHAPE, c + ": " + name + " must be aligned to its element type");
   return SB_OK;
 }
 
@@ -714,7 +730,10 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
   if (ld_f > MAX_LD || ld_f < (order == SB_COLUMN_MAJOR ? n : d))
     return fail(SB_E_SHAPE, c + ": ld_f must be >= n (column-major) or >= d (row-major)");
   if (k > 0 && (ld_top < n || ld_top > MAX_LD)) return fail(SB_E_SHAPE, c + ": ld_top must be >= n");
-  if (!aligned(F, dtype == SB_F32 ? 4 : 2)) return fail(SB_E_SHAPE, c + ": F must be aligned to its element type");
+  if (const char* name = misaligned({{"F", F, uintptr_t(dtype == SB_F32 ? 4 : 2)}, {"labels", logp || rank ? labels : nullptr, 4},
+                                     {"logp", logp, 4}, {"rank", rank, 4}, {"lse", lse, 4}, {"entropy", entropy, 4},
+                                     {"top_id", k > 0 ? top_id : nullptr, 4}, {"top_logp", k > 0 ? top_logp : nullptr, 4}}))
+    return fail(SB_E_SHAPE, c + ": " + name + " must be aligned to its element type");
   const int32_t rc = need_ws(ws, ws_bytes, log_probs_ws_bytes(n, d, k), "sb_log_probs");
   if (rc) return rc;
   return launch_log_probs(F, dtype, order, n, d, ld_f, temperature, logp || rank ? labels : nullptr, logp, rank, lse,
