@@ -162,13 +162,13 @@ __device__ inline void add_targets(const Listed* ent, int K, int rl, int jg, flo
 #pragma unroll
     for (int u = 0; u < 8; ++u) p[u] = ent[(s + u) * ROWS + rl];
 #pragma unroll
-    for (int u = 0; u < 8; ++u) put_target<CG>(trow, seen, (uint32_t)(p[u].id - jg), wt * p[u].e);
+    for (int u = 0; u < 8; ++u) put_target<CG>(trow, seen, column_from(p[u].id, jg), wt * p[u].e);
   }
   for (; s < K; ++s) {
     const Listed p = ent[s * ROWS + rl];
-    put_target<CG>(trow, seen, (uint32_t)(p.id - jg), wt * p.e);
+    put_target<CG>(trow, seen, column_from(p.id, jg), wt * p.e);
   }
-  if (y >= 0) put_target<CG>(trow, seen, (uint32_t)(y - jg), A);
+  if (y >= 0) put_target<CG>(trow, seen, column_from(y, jg), A);
 }
 
 // Squared norms of a tile's columns: CG lanes take the columns of a segment's rows,
@@ -946,7 +946,7 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, in
     uint64_t mine = 0;
 #pragma unroll 8
     for (int s = 0; s < K; ++s)
-      mine |= (uint64_t)((uint32_t)(ent[s * 64 + lane].id - j0) < (uint32_t)(cols > 0 ? cols : 0)) << s;
+      mine |= (uint64_t)(column_from(ent[s * 64 + lane].id, j0) < (uint32_t)(cols > 0 ? cols : 0)) << s;
     // 16 columns from c0; all of them exist (FULL), or those up to `last`
     auto group = [&](auto full, int c0, int last) {
       constexpr bool FULL = decltype(full)::value;
@@ -964,11 +964,11 @@ __global__ void __launch_bounds__(64 * WIDE_WAVES) k_distill_range(RowArgs r, in
         const int s = __builtin_ctzll(left);
         left &= left - 1;
         const Listed p = ent[s * 64 + lane];
-        const uint32_t c = (uint32_t)(p.id - j0 - c0);
+        const uint32_t c = column_from(p.id, j0 + c0);
         if (c < 16) mine &= ~(uint64_t(1) << s);
         put_target<16>(trow, seen, c, p.e);
       }
-      if (y >= 0) put_target<16>(trow, seen, (uint32_t)(y - j0 - c0), A);
+      if (y >= 0) put_target<16>(trow, seen, column_from(y, j0 + c0), A);
       float* Gc = a.G + (int64_t)(j0 + c0) * a.ld_g + base;
       float* Hc = MODE == 2 && a.hess ? a.hess + (int64_t)(j0 + c0) * a.ld_h + base : nullptr;
 #pragma unroll

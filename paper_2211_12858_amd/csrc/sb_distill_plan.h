@@ -13,6 +13,10 @@ constexpr int DISTILL_ONE_PART_D = 512;
 constexpr int64_t DISTILL_NEAR_LD = int64_t(1) << 24;
 constexpr int DISTILL_RED = 8;  // per-wave values that a block's waves exchange
 
+// A class's column counted from column j0, unsigned: classes before j0 and those that no
+// row has (any int32) come out at 2^31 or more, or past the last column.
+constexpr uint32_t column_from(int32_t id, int32_t j0) { return (uint32_t)id - (uint32_t)j0; }
+
 // Rows in the registers of a block's waves.
 struct DistillPlan {
   int rows;    // rows per tile; a wave takes 64 / rows sets of c columns of each
