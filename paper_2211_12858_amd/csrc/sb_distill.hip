@@ -222,11 +222,14 @@ struct WaveTile {
     }
   }
   __device__ void load(float (&x)[C], int64_t base, uint32_t loc) const {
-    const float* p = a.F + (int64_t)j0 * a.ld_f + base;
+    int64_t ld = a.ld_f;
+    const float* p = a.F + (int64_t)j0 * ld + base;
 #pragma unroll
     for (int i = 0; i < C; ++i) {
-      x[i] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + at(i, loc, a.ld_f));
-      if (STEP && (FULLC || i < last)) p += a.ld_f;
+      // seen anew at every step: 64-bit offsets of all columns would otherwise be formed ahead and held, spilled
+      if (sizeof(OFF) == 8) asm volatile("" : "+s"(ld));
+      x[i] = *reinterpret_cast<const float*>(reinterpret_cast<const char*>(p) + at(i, loc, ld));
+      if (STEP && (FULLC || i < last)) p += ld;
     }
   }
   __device__ void put(int q, float v) const { red[(q * W + w) * 64 + lane] = v; }
