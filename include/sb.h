@@ -527,7 +527,8 @@ int32_t sb_update_and_gradients(int32_t loss, float* F, int64_t n, int32_t d, in
  * nor each other.
  * Sums in fp32 of terms at the row's maximum; ranks and the order of the
  * alternatives compare the scores as given, so they are exact.
- * Workspace: sb_workspace_bytes(SB_CALL_LOG_PROBS, n, d, k).
+ * Workspace: sb_workspace_bytes(SB_CALL_LOG_PROBS, n, d, k) for
+ * SB_COLUMN_MAJOR; SB_ROW_MAJOR needs none.
  */
 int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int32_t d, int64_t ld_f,
                      double temperature, const int32_t* labels, float* logp, int32_t* rank, float* lse, float* entropy,

@@ -734,7 +734,8 @@ int32_t sb_log_probs(const void* F, int32_t dtype, int32_t order, int64_t n, int
                                      {"logp", logp, 4}, {"rank", rank, 4}, {"lse", lse, 4}, {"entropy", entropy, 4},
                                      {"top_id", k > 0 ? top_id : nullptr, 4}, {"top_logp", k > 0 ? top_logp : nullptr, 4}}))
     return fail(SB_E_SHAPE, c + ": " + name + " must be aligned to its element type");
-  const int32_t rc = need_ws(ws, ws_bytes, log_probs_ws_bytes(n, d, k), "sb_log_probs");
+  // only column-major rows are split, and leave partial results
+  const int32_t rc = need_ws(ws, ws_bytes, order == SB_COLUMN_MAJOR ? log_probs_ws_bytes(n, d, k) : 0, "sb_log_probs");
   if (rc) return rc;
   return launch_log_probs(F, dtype, order, n, d, ld_f, temperature, logp || rank ? labels : nullptr, logp, rank, lse,
                           entropy, k, top_id, top_logp, ld_top, ws, static_cast<hipStream_t>(stream));

@@ -11,9 +11,9 @@
 //   time: a running maximum, the two sums rescaled when it grows, and the best classes
 //   so far as a sorted list in registers; a score enters it if it is above the last one
 //   (equal scores stay behind the earlier class).  Column-major scores are read as runs
-//   of a column; row-major ones go through an LDS tile of 128 bytes of 64 rows.  Where
-//   there are few rows the columns are split over waves, and k_join joins the partial
-//   statistics and lists.
+//   of a column; where there are few rows the columns are split over waves, and k_join
+//   joins the partial statistics and lists.  Row-major ones go through an LDS tile of
+//   128 bytes of 64 rows, unsplit.
 // k_row_in_block (row-major): a row in the registers of a wave or of a block.  The
 //   k-th largest of the threads' maxima bounds the k-th largest score from below; the
 //   scores not under it, seldom many more than k, are collected in LDS and ranked
@@ -51,8 +51,9 @@ struct LogProbArgs {
   int32_t* top_id;
   float* top_logp;
   int64_t ld_top;
-  int tiles, splits, per;  // k_rows_by_lane: row tiles, column splits, columns per split
-  double* part;            // splits > 1: [split][2 + k][n]: (m, s), (t, before), the list
+  int tiles;        // of 64 rows: k_cols_by_lane, k_rows_by_lane
+  int splits, per;  // k_cols_by_lane: column splits, columns per split
+  double* part;     // splits > 1: [split][2 + k][n]: (m, s), (t, before), the list
 };
 
 __device__ inline float exp2_hw(float x) { return __builtin_amdgcn_exp2f(x); }

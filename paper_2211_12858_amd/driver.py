@@ -103,7 +103,8 @@ def log_probs(scores, labels=None, k=0, temperature=1.0, order="column", stream=
         def new(dtype, *shape):
             return torch.empty(shape, dtype=dtype, device=dev)
 
-        ws = workspace(L.sb_workspace_bytes(L.SB_CALL_LOG_PROBS, n=n, d=d, k=k), dev)
+        ws_bytes = L.sb_workspace_bytes(L.SB_CALL_LOG_PROBS, n=n, d=d, k=k)
+        ws = workspace(ws_bytes if order == "column" else 0, dev)
         r = LogProbs(logp=None if labels is None else new(torch.float32, n),
                      rank=None if labels is None else new(torch.int32, n),
                      lse=new(torch.float32, n), entropy=new(torch.float32, n),
