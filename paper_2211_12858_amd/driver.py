@@ -76,6 +76,14 @@ def _on(device, stream):
             yield
 
 
+def _hold(*tensors):
+    """What the current stream's work reads: its memory goes to no other tensor before that work is done, whoever drops
+    the tensor."""
+    for t in tensors:
+        if t is not None:
+            t.record_stream(torch.cuda.current_stream(t.device))
+
+
 def _check_vector(name, t, n, dtype, device):
     if t.shape != (n,) or t.dtype != dtype or not t.is_contiguous() or t.device != device:
         raise ValueError("%s must be %d contiguous elements of %s on %s" % (name, n, dtype, device))
@@ -357,7 +365,8 @@ class Booster:
 
         t_id, t_val: (k, n) int32 classes and float32 values, as ``log_probs`` returns them (device tensors; places of
         class -1 are unused); values: "log_probs" (at this temperature) or "logits"; labels: (n,) int32, needed for a
-        hard_weight above 0."""
+        hard_weight above 0.  Steps on another stream keep what they read until they are done, also when other lists
+        are set meanwhile; a captured step reads these lists again whenever it is replayed, so keep them for it."""
         if self.loss != "distill":
             raise ValueError("only the loss 'distill' has a teacher")
         k = t_id.shape[0] if t_id.dim() == 2 else 0
@@ -368,8 +377,8 @@ class Booster:
             _check_vector("labels", labels, self.n, torch.int32, self._F.device)
         elif hard_weight > 0:
             raise ValueError("a hard_weight above 0 needs labels")
-        ws = workspace(L.sb_workspace_bytes(L.SB_CALL_DISTILL, n=self.n, d=self.d, k=k), self._F.device)
-        self.teacher = (float(temperature), float(hard_weight), labels, L.TEACHER[values], k, t_id, t_val, ws)
+        ws_bytes = L.sb_workspace_bytes(L.SB_CALL_DISTILL, n=self.n, d=self.d, k=k)
+        self.teacher = (float(temperature), float(hard_weight), labels, L.TEACHER[values], k, t_id, t_val, ws_bytes)
 
     def _teacher(self):
         if self.teacher is None:
@@ -378,11 +387,13 @@ class Booster:
 
     def distill_loss(self, stream=None):
         """The distillation loss of every row at the current scores: a new (n,) float32 tensor."""
-        T, w, y, kind, k, t_id, t_val, ws = self._teacher()
+        T, w, y, kind, k, t_id, t_val, ws_bytes = self._teacher()
         self.flush(stream)
         with _on(self._F.device, stream):
+            ws = workspace(ws_bytes, self._F.device)
             loss = torch.empty(self.n, dtype=torch.float32, device=self._F.device)
             L.sb_distill_loss(self._F, self.n, self.d, self.n, T, w, y, kind, k, t_id, t_val, self.n, loss, ws, ws.numel())
+            _hold(y, t_id, t_val)
         return loss
 
     def log_probs(self, labels=None, k=0, temperature=1.0, stream=None):
@@ -394,10 +405,13 @@ class Booster:
         """Derivatives at the current scores (a held update is applied first, in the same pass)."""
         n, d = self.n, self.d
         if self.loss == "distill":
-            T, w, y, kind, k, t_id, t_val, ws = self._teacher()
+            T, w, y, kind, k, t_id, t_val, ws_bytes = self._teacher()
             self.flush(stream)
-            L.sb_distill_gradients(self._F, n, d, n, T, w, y, kind, k, t_id, t_val, n, None, self.G, n, self.hess, n, None,
-                                   self.norm2, ws, ws.numel(), stream)
+            with _on(self._F.device, stream):
+                ws = workspace(ws_bytes, self._F.device)
+                L.sb_distill_gradients(self._F, n, d, n, T, w, y, kind, k, t_id, t_val, n, None, self.G, n, self.hess, n,
+                                       None, self.norm2, ws, ws.numel())
+                _hold(y, t_id, t_val)
             return
         h_row = self.h_row if self.loss == "sigmoid" else None
         if self.pending is not None:
