@@ -369,6 +369,8 @@ class Booster:
         are set meanwhile; a captured step reads these lists again whenever it is replayed, so keep them for it."""
         if self.loss != "distill":
             raise ValueError("only the loss 'distill' has a teacher")
+        if values not in tuple(L.TEACHER):
+            raise ValueError("values must be 'log_probs' or 'logits'")
         k = t_id.shape[0] if t_id.dim() == 2 else 0
         for t, dtype in ((t_id, torch.int32), (t_val, torch.float32)):
             if t.shape != (k, self.n) or t.dtype != dtype or not t.is_contiguous() or t.device != self._F.device:
