@@ -390,8 +390,8 @@ class Booster:
     def distill_loss(self, stream=None):
         """The distillation loss of every row at the current scores: a new (n,) float32 tensor."""
         T, w, y, kind, k, t_id, t_val, ws_bytes = self._teacher()
-        self.flush(stream)
         with _on(self._F.device, stream):
+            self.flush()
             ws = workspace(ws_bytes, self._F.device)
             loss = torch.empty(self.n, dtype=torch.float32, device=self._F.device)
             L.sb_distill_loss(self._F, self.n, self.d, self.n, T, w, y, kind, k, t_id, t_val, self.n, loss, ws, ws.numel())
@@ -400,16 +400,17 @@ class Booster:
 
     def log_probs(self, labels=None, k=0, temperature=1.0, stream=None):
         """What the current scores answer (:func:`log_probs`)."""
-        self.flush(stream)
-        return log_probs(self._F, labels, k, temperature, "column", stream)
+        with _on(self._F.device, stream):
+            self.flush()
+            return log_probs(self._F, labels, k, temperature)
 
     def gradients(self, stream=None):
         """Derivatives at the current scores (a held update is applied first, in the same pass)."""
         n, d = self.n, self.d
         if self.loss == "distill":
             T, w, y, kind, k, t_id, t_val, ws_bytes = self._teacher()
-            self.flush(stream)
             with _on(self._F.device, stream):
+                self.flush()
                 ws = workspace(ws_bytes, self._F.device)
                 L.sb_distill_gradients(self._F, n, d, n, T, w, y, kind, k, t_id, t_val, n, None, self.G, n, self.hess, n,
                                        None, self.norm2, ws, ws.numel())

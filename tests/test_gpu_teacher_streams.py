@@ -1,4 +1,6 @@
 """A booster's lists and workspace stay until the work that reads them is done, on whatever stream it runs."""
+import contextlib
+
 import numpy as np
 import pytest
 import torch
@@ -6,6 +8,7 @@ import torch
 pytestmark = pytest.mark.gpu
 
 import gpu_util as gu  # noqa: E402
+from paper_2211_12858_amd import driver  # noqa: E402
 from paper_2211_12858_amd.driver import Booster  # noqa: E402
 
 
@@ -85,3 +88,39 @@ def test_captured_and_replayed(d):
         gu.sync()
         assert torch.equal(a.G, b.G) and torch.equal(a.hess, b.hess) and torch.equal(a.norm2, b.norm2), rep
         assert torch.equal(loss, want), rep
+
+
+def test_a_held_update_goes_where_the_call_goes(monkeypatch):
+    """The held update and the call that reads its scores run on one device and stream, whichever are current outside."""
+    rng = np.random.default_rng(4)
+    n, d = 500, 12
+    b = Booster(rng.integers(0, 16, (n, 4)).astype(np.uint8), 16, d, "distill", "top_outputs", 3, 2, device=gu.DEV)
+    b.set_teacher(gu.up(rng.integers(0, d, (3, n)).astype(np.int32)), gu.up(rng.normal(size=(3, n)).astype(np.float32)))
+    inside, kept_on = [], driver._on
+
+    @contextlib.contextmanager
+    def on(device, stream):
+        with kept_on(device, stream):
+            inside.append(device)
+            yield
+            inside.pop()
+
+    updates, kept = [], driver.L.sb_update_predictions
+
+    def update(*args):
+        updates.append(list(inside))
+        return kept(*args)
+
+    monkeypatch.setattr(driver, "_on", on)
+    monkeypatch.setattr(driver.L, "sb_update_predictions", update)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    for call in (b.gradients, b.distill_loss, b.log_probs):
+        for stream in (None, s, s.cuda_stream):
+            gu.sync()
+            b.step()
+            gu.sync()
+            call(stream=stream)
+            assert b.pending is None
+    gu.sync()
+    assert len(updates) == 9 and all(u and u[0] == b._F.device for u in updates)
