@@ -328,9 +328,10 @@ class Booster:
         self.h_row = torch.empty(n, dtype=torch.float32, device=dev)
         self.ones = torch.ones(n, dtype=torch.float32, device=dev)
         self.norm2 = torch.zeros(d, dtype=torch.float64, device=dev)
-        self.ws_grad = workspace(L.sb_workspace_bytes(L.SB_CALL_GRADIENTS, n=n, d=d), dev)
         self.ws_upd = workspace(L.sb_workspace_bytes(L.SB_CALL_UPDATE_PREDICTIONS, n=n), dev)
-        self.ws_upd_grad = workspace(L.sb_workspace_bytes(L.SB_CALL_UPDATE_AND_GRADIENTS, n=n, d=d), dev)
+        if loss != "distill":  # whose calls take theirs with every call
+            self.ws_grad = workspace(L.sb_workspace_bytes(L.SB_CALL_GRADIENTS, n=n, d=d), dev)
+            self.ws_upd_grad = workspace(L.sb_workspace_bytes(L.SB_CALL_UPDATE_AND_GRADIENTS, n=n, d=d), dev)
         self.labels = None
         self.Y = None
         self.hess = torch.empty((d, n), dtype=torch.float32, device=dev) if loss == "distill" else None

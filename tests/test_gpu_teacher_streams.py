@@ -124,3 +124,23 @@ def test_a_held_update_goes_where_the_call_goes(monkeypatch):
             assert b.pending is None
     gu.sync()
     assert len(updates) == 9 and all(u and u[0] == b._F.device for u in updates)
+
+
+def test_only_what_the_loss_uses_is_allocated(monkeypatch):
+    rng = np.random.default_rng(4)
+    bins = rng.integers(0, 16, (300, 4)).astype(np.uint8)
+    asked, kept = [], driver.L.sb_workspace_bytes
+    monkeypatch.setattr(driver.L, "sb_workspace_bytes", lambda call, **kw: asked.append(call) or kept(call, **kw))
+    other = {driver.L.SB_CALL_GRADIENTS, driver.L.SB_CALL_UPDATE_AND_GRADIENTS}
+    for loss in ("softmax", "sigmoid"):
+        asked.clear()
+        Booster(bins, 16, 12, loss, "top_outputs", 3, 2, device=gu.DEV)
+        assert other <= set(asked)
+    asked.clear()
+    b = Booster(bins, 16, 12, "distill", "top_outputs", 3, 2, device=gu.DEV)
+    b.set_teacher(torch.zeros((2, 300), dtype=torch.int32, device=gu.DEV), torch.zeros((2, 300), device=gu.DEV))
+    for _ in range(2):
+        b.step()
+    b.flush()
+    gu.sync()
+    assert not other & set(asked)
