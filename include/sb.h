@@ -75,6 +75,8 @@
 extern "C" {
 #endif
 
+/* Raised when a call that exists changes.  sb_log_probs, sb_distill_loss and
+ * sb_distill_gradients came in under 4, with no change to the others. */
 #define SB_ABI_VERSION 4
 
 /* Status codes. */

@@ -22,20 +22,20 @@
 //   the targets in that tile, from which 16 lanes per row segment add the squared
 //   column norms in fp64, in a fixed order; a block's sums are one partial.  While a
 //   tile's gradients go out the same registers take the next tile's scores.
-//   2M x 100 with labels and 10 places 403 us, 4.4 TB/s of 4.7 in a copy: the bytes.
+//   2M x 100 with labels and 10 places 402 us, 4.4 TB/s of 4.7 in a copy: the bytes.
 //   300,007 x 1000 with hessians and 32 places 1280 us, 2.9 TB/s: one block of 16
 //   waves per CU holds 32 rows, and columns of an odd number of rows start anywhere in
 //   a cache line, so that half as many requests again go to the L2 (300,032 rows 950 us);
 //   vector instructions take a third of the issue slots.
-//   The loss alone: 1,000,003 x 100 with 10 places 107 us, 4.5 TB/s: the bytes (134 us
+//   The loss alone: 1,000,003 x 100 with 10 places 104 us, 4.7 TB/s: the bytes (134 us
 //   with the listed scores read from memory).
 // k_loss_by_lane: the loss alone of many rows with short lists, a wave per tile.
 // k_distill_stats, k_distill_rows, k_distill_range (wider rows): maxima and sums of
 //   column ranges, then every row's statistics, targets and loss, then the outputs range
 //   by range, with what each range's targets take off the loss (k_distill_join adds
 //   them up; listed scores read from memory in k_distill_rows took 86 us more).  F is
-//   read twice; 20,001 x 5003 with hessians and 64 places 111, 12 and 261 us, the last
-//   4.6 TB/s.
+//   read twice; 20,001 x 5003 with hessians and 64 places 455 us in all, of which 131, 11
+//   and 294, the last 4.1 TB/s.
 //
 // k_hot_loss (with k_hot_stats): the loss at T > 4, whose terms are far larger than what
 //   they add up to.
@@ -1070,8 +1070,8 @@ __global__ void __launch_bounds__(256) k_distill_join(const float* sums, int ran
 // exponential itself is as small as its roundings ask for.  The list's exponentials and
 // all sums and logarithms of a row are fp64.
 // Up to T = HOT the fp32 forms above lose at most four bits more than they do at T = 1.
-// Bound by vector instructions (some 25 per score, two of them in fp64) and, in lists of
-// many rows, by the listed scores, a cache line each: 1,000,003 x 100 with 10 places
+// Bound by vector instructions (some 35 per score, two of them in fp64; 0.7 of the issue
+// slots at 20,001 x 5003) and, in lists of many rows, by the listed scores, a cache line each: 1,000,003 x 100 with 10 places
 // 213 us (107 by the fp32 form), 300,007 x 1000 with 25 397 (342), 20,001 x 5003 with 64
 // 170 (111); 64 x 60,000 37 (23), of which a second launch is part.  A call for gradients
 // reads the scores once more for it.
@@ -1335,8 +1335,11 @@ void launch_hot(const RowArgs& r, void* ws, bool mix, hipStream_t st) {
 
 // The loss alone, a wave per tile: where there are tiles for the waves of the card, and
 // few listed scores, which by then are read from memory once more, a cache line each (us
-// by lane and by blocks: 100,000 x 1000 with 10 places 85 and 118, x 400 42 and 54;
-// 300,007 x 1000 with 32 377 and 387; 1M x 200 with 5 198 and 188, x 100 with 10 157 and 107).
+// by lane and by blocks: 100,000 x 1000 with 10 places 86 and 118, with 25 113 and 120,
+// x 400 with 10 42 and 53; 300,007 x 1000 with 25 349 and 380, with 32 387 and 388; 1M x
+// 400 with 4 331 and 395, x 100 with 2 99 and 101, x 100 with 10 156 and 109; 100,003 x
+// 1500 with 37 176 and 207).  It gives away 4% at 1M x 200 with 5 (199 and 192), and more
+// where there are fewer rows (50,000 x 400 with 4 20 and 31).
 bool loss_by_lane(const DistillArgs& a) { return a.n >= 100000 && a.d >= 40 * a.k; }
 
 template <int ROWS, int C, int MODE, typename OFF>

@@ -991,9 +991,13 @@ void launch_rows(LogProbArgs a, hipStream_t st) {
   // A lane per row where there are rows for the lanes of the card: its time is that of
   // d columns until there are some 100,000 rows, a wave's that of the rows.  16-bit
   // scores are half the bytes for a wave and the same work for a lane.  (us by lane and
-  // by wave: fp32, 5 alternatives, 20,000 x 125 20 and 19, 50,000 x 312 40 and 46,
-  // 200,000 x 640 134 and 189; fp16, 16 alternatives, 20,000 x 125 29 and 24, 200,000 x
-  // 640 238 and 206, 200,000 x 300 137 and 180, 500,000 x 600 399 and 504.)
+  // by wave: fp32, 5 alternatives, 20,000 x 125 20 and 20, 50,000 x 312 41 and 46,
+  // 200,000 x 640 134 and 189, x 1000 246 and 212; 64 alternatives, 100,000 x 300 108 and
+  // 233, 200,000 x 640 313 and 487; fp16, 16 alternatives, 20,000 x 125 30 and 24, 200,000
+  // x 300 138 and 180, x 640 238 and 208, 500,000 x 600 400 and 508, x 1000 596 and 515; 64
+  // alternatives, 500,000 x 600 720 and 1155.)  The limit of 640 columns is the same for
+  // every size and list: 200,000 x 800 fp32 with 5 is taken by wave, 204, where a lane per
+  // row takes 162.
   if (a.n >= (int64_t)(sizeof(T) == 2 ? 480 : 160) * a.d && a.d <= 640) {
     by_list<RowsByLane<T>::template With>(a.k, a, dim3((a.tiles + 3) / 4), st);
     return;
