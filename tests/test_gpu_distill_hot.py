@@ -15,11 +15,15 @@ A factor of 2 on the whole for second-order terms.
 """
 import numpy as np
 import pytest
+import torch
 
 from oracle import scores as osc
 
 pytestmark = pytest.mark.gpu
 
+import gpu_util as gu  # noqa: E402
+from paper_2211_12858_amd import _lib as L  # noqa: E402
+from paper_2211_12858_amd.driver import workspace  # noqa: E402
 from test_gpu_distill import run  # noqa: E402
 
 U = 2.0 ** -24
@@ -160,3 +164,58 @@ def test_forward_and_gradient_calls_agree():
         _, part = run(F, ids, vals, 50.0, 0.0, None, "logits", loss=False)
         for name in part:
             assert np.array_equal(part[name], got[name]), name
+
+
+@pytest.mark.parametrize("n,d,k,ld", [(70, 20, 5, 3), (65, 700, 9, 5), (5, 3001, 6, 3), (70, 9, 3, (1 << 27) + 1)])
+def test_strides_and_offsets_past_32_bits(n, d, k, ld):
+    rng = np.random.default_rng(n + d)
+    F = rng.normal(size=(n, d)).astype(np.float32)
+    ids, vals = teacher_lists(rng, F, k, 50.0, "logits", 0.5)
+    plain, _ = run(F, ids, vals, 50.0, 0.0, None, "logits")
+    fwd, got = run(F, ids, vals, 50.0, 0.0, None, "logits", ld=ld)
+    assert np.array_equal(fwd, plain) and np.array_equal(got["loss"], plain)
+
+
+@pytest.mark.parametrize("d", [5, 100, 1600])
+def test_nan_and_inf_stay_in_their_row(d):
+    rng = np.random.default_rng(d)
+    F = rng.normal(size=(70, d)).astype(np.float32)
+    ids, vals = teacher_lists(rng, F, 5, 10.0, "logits", 0.5)
+    y = rng.integers(0, d, 70).astype(np.int32)
+    want, _ = run(F, ids, vals, 10.0, 0.3, y, "logits")
+    F[3, 0], F[64, d - 1], F[69, 2], vals[1, 20] = np.nan, np.inf, np.nan, np.nan
+    fwd, _ = run(F, ids, vals, 10.0, 0.3, y, "logits")
+    keep = np.setdiff1d(np.arange(70), [3, 20, 64, 69])
+    assert np.array_equal(fwd[keep], want[keep])
+
+
+@pytest.mark.parametrize("n,d", [(300, 100), (200, 1500)])
+def test_captured_and_replayed(n, d):
+    """Replayed on changed scores between eager work; one workspace each for the graph and the eager calls."""
+    print("case: hot graph", n, d, flush=True)
+    rng = np.random.default_rng(d)
+    F0 = rng.normal(size=(n, d)).astype(np.float32)
+    ids, vals = teacher_lists(rng, F0, 5, 20.0, "log_probs", 0.5)
+    M, idd, vd = torch.zeros((d, n), device=gu.DEV), gu.up(ids), gu.up(vals)
+    loss, G = torch.zeros(n, device=gu.DEV), torch.zeros((d, n), device=gu.DEV)
+    ws = workspace(L.sb_workspace_bytes(L.SB_CALL_DISTILL, n=n, d=d, k=5), gu.DEV)
+
+    def call():
+        L.sb_distill_gradients(M, n, d, n, 20.0, 0.0, None, 1, 5, idd, vd, n, loss, G, n, None, 0, None, None, ws, ws.numel())
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    gu.sync()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for rep in range(3):
+        F = rng.normal(size=(n, d)).astype(np.float32)
+        M.copy_(gu.up(np.ascontiguousarray(F.T)))
+        g.replay()
+        gu.sync()
+        _, eager = run(F, ids, vals, 20.0, 0.0, None, "log_probs", hess=False, row=False, norms=False)
+        assert np.array_equal(loss.cpu().numpy(), eager["loss"]) and np.array_equal(G.cpu().numpy(), eager["G"]), rep
